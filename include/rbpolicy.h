@@ -28,6 +28,14 @@
  *   rb_asymre_coef,          AsymRE: coefficient at insert and the
  *   policy_asymre_fwd_bwd    objective with its gradient                (App. D.2)
  *
+ * and, not in the paper, what stands before and after it at the same vocabulary:
+ *
+ *   policy_verify_drafts     tokens from drafts and the policy's logits, with the
+ *                            behaviour log-probs that rb_push records
+ *   policy_embed_fwd,        a batch's embedding rows, and the table's gradient,
+ *   policy_embed_bwd         which a tied head shares with d loss / d W
+ *   policy_distill_fwd_bwd   divergence from a teacher's top logits, and its gradient
+ *
  * Conventions shared by every entry point:
  *   - Pointers marked "device" are HIP device pointers (or managed memory); the
  *     structs themselves and every scalar argument live on the host.
@@ -102,7 +110,16 @@ enum {
   RBP_OP_LOGPROB_BWD = 4,   /* n = tokens per backward chunk (T for one chunk) */
   RBP_OP_LOSS_SEQ = 5,      /* n = B, sequences of policy_loss_seq_fwd_bwd     */
   RBP_OP_FUSED = 6,         /* n = tokens per policy_fused_fwd_bwd chunk       */
-  RBP_OP_NOTE_USE = 7       /* n = capacity of the record table              */
+  RBP_OP_NOTE_USE = 7,      /* n = capacity of the record table              */
+  RBP_OP_EMBED_BWD = 8,     /* n = T                                          */
+  RBP_OP_DISTILL = 9,       /* n = T, d = K (teacher entries per token)       */
+  RBP_OP_VERIFY = 10        /* n = B, d = K (drafts per sequence)             */
+};
+
+/* ---- element types of logits and of policy_embed_bwd's dx -------------------- */
+enum {
+  RBP_BF16 = 0,
+  RBP_F32 = 1
 };
 
 /*
@@ -518,6 +535,126 @@ int rb_note_use(const int32_t* idx, int64_t n_draw, int64_t head, int64_t capaci
  */
 int rb_hist_accumulate(const int32_t* values, int64_t n, int32_t lo, int32_t n_bins,
                        int64_t* hist, void* stream);
+
+/*
+ * Embedding lookup: out_t = scale * table[tokens_t], rounded to bf16 once.
+ * table   device bf16 [V, d] (W where the head is tied); tokens device int32 [T];
+ * seq_of_token device int32 [T] or NULL: a negative entry masks the token (a zero
+ *         row); a token outside [0, V) that is not masked gives a row of NaN;
+ * out     device bf16 [T, d], overwritten.
+ * Errors: RBP_EINVAL (null pointers, T < 0, d < 1, V < 1, scale not finite);
+ *         RBP_EUNSUPPORTED (d % 8 != 0, table or out not aligned to 16 bytes,
+ *         T above 2^31 - 1).
+ */
+int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
+                     const int32_t* seq_of_token, int64_t T, int32_t d, int32_t V,
+                     float scale, uint16_t* out, void* stream);
+
+/*
+ * Its backward: dW_v (+)= scale * sum over {t: tokens_t = v, not masked} of dx_t.
+ * The tokens are sorted (stably) and each row's sum runs over its tokens in
+ * batch order, in pieces of a fixed number of sorted positions: fp32, no
+ * atomics on it, no dependence on how often a token occurs.
+ * dx      device [T, d], RBP_BF16 or RBP_F32 (dx_type); tokens, seq_of_token as in
+ *         policy_embed_fwd (masked tokens and those outside [0, V) add nothing);
+ * dW      device fp32 [V, d]: overwritten (rows without a token: 0), or added to
+ *         when accumulate_dW != 0 (rows without a token are left as they are) --
+ *         with a tied head, the dW of policy_logprob_bwd or policy_fused_fwd_bwd.
+ * ws      device, >= rbp_workspace_bytes(RBP_OP_EMBED_BWD, T, d, V).
+ * Errors: RBP_EINVAL (null pointers, T < 0, d < 1, V < 1, an unknown dx_type, scale
+ *         not finite); RBP_EUNSUPPORTED (d % 8 != 0, dx or dW not aligned to 16
+ *         bytes, T above 2^30); RBP_EWORKSPACE.
+ */
+int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
+                     const int32_t* seq_of_token, int64_t T, int32_t d, int32_t V,
+                     float scale, float* dW, int accumulate_dW, void* ws, size_t ws_bytes,
+                     void* stream);
+
+/*
+ * Verification of drafted tokens (speculative sampling): what is emitted is
+ * distributed as if every token had been sampled from the policy.  With
+ * p_k = softmax(logits_k / temperature), q_k = softmax(draft_logits_k /
+ * temperature) and n_i = n_draft[i] drafts x_0 .. of sequence i:
+ *   draft k is accepted iff u_k q_k(x_k) < p_k(x_k); a is the first that is not
+ *   (n_i if all are);
+ *   the token after the accepted ones is drawn with weights max(p_a - q_a, 0) if
+ *   a < n_i (p_a if these are all 0), p_a if a = n_i: it is the least v whose
+ *   running sum of weights exceeds u_K times their total.
+ * Without drafts (K = 0) this samples one token per sequence.
+ * logits  device [B * (K + 1), V], rows `ld` elements apart (ld >= V): row
+ *         i (K + 1) + k is the policy's at position k of sequence i;
+ * draft_logits device [B * K, V] of the same type, rows `ld_draft` apart, or NULL:
+ *         the drafts were not sampled (copied from earlier text, say), so
+ *         q_k is 1 at x_k and 0 elsewhere;
+ * logits_type RBP_BF16 or RBP_F32;
+ * draft_tokens device int32 [B, K]; a draft outside [0, V) is rejected;
+ * n_draft device int32 [B] or NULL (K each): clamped to at most K; a negative entry
+ *         marks a sequence that takes no part (n_out = 0, its logits are not used);
+ * u       device fp32 [B, K + 1], in [0, 1): the K acceptance tests' and the
+ *         draw's random numbers;
+ * out_tokens device int32 [B, K + 1]: accepted drafts, the drawn token, then -1;
+ * out_logp device fp32 [B, K + 1]: log p of each emitted token (the behaviour
+ *         log-prob for rb_push), then 0;
+ * n_out   device int32 [B]: tokens emitted, a + 1.
+ * Sums, comparisons and the search for the drawn token are carried out in 64 bits,
+ * so a decision differs from the exact one only where a border lies within about
+ * 1e-12 of u.  Logits of -infinity have probability 0.  A row of logits with a NaN,
+ * with +infinity, or with -infinity only has no distribution: a draft at such a
+ * position of the policy's is rejected, and drawing there emits token -1 with a
+ * NaN log-prob; such a row of draft_logits has its draft rejected, and the token
+ * is drawn from p_a.
+ * ws      device, >= rbp_workspace_bytes(RBP_OP_VERIFY, B, K, V).
+ * Errors: RBP_EINVAL (null pointers, B < 0, K < 0, V < 1, ld or ld_draft < V, an
+ *         unknown type, temperature not positive and finite, logits not aligned
+ *         to their type); RBP_EUNSUPPORTED (K above 255, B (K + 1) above 2^24);
+ *         RBP_EWORKSPACE.
+ */
+int policy_verify_drafts(const void* logits, const void* draft_logits, int logits_type,
+                         int64_t ld, int64_t ld_draft, const int32_t* draft_tokens,
+                         const int32_t* n_draft, const float* u, int32_t B, int32_t K,
+                         int32_t V, float temperature, int32_t* out_tokens,
+                         float* out_logp, int32_t* n_out, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/*
+ * Distillation from a teacher's top K logits per token, and its gradient to the
+ * policy's logits z (of any head):
+ *   l_k     = teacher_logits_k / temperature over the entries with an id >= 0;
+ *   p       = softmax(l), or exp(l - teacher_lse_t) when teacher_lse is given (the
+ *             teacher's log-sum-exp over its whole vocabulary, at this
+ *             temperature: the entries keep their mass P = sum_k p_k <= 1);
+ *   KL_t    = sum_k p_k (log p_k - log softmax(z / temperature)_{id_k});
+ *   loss   += scale * sum_t KL_t / (n_seq_total * seq_len_i)   (i = seq_of_token[t]);
+ *   dz_{t,v} = scale / (n_seq_total * seq_len_i * temperature)
+ *              * (P softmax(z / temperature)_v - sum_{k: id_k = v} p_k).
+ * logits  device [T, V], RBP_BF16 or RBP_F32 (logits_type), rows `ld` elements apart
+ *         (ld >= V);
+ * teacher_ids device int32 [T, K] (an entry < 0 is absent; an id that occurs twice
+ *         counts twice); teacher_logits device fp32 [T, K]; teacher_lse device fp32
+ *         [T] or NULL;
+ * seq_of_token, seq_len, n_seq_total as in policy_loss_fwd_bwd; a masked token
+ *         (seq_of_token < 0) has KL 0 and a zero gradient, whatever its logits and
+ *         teacher hold.  So does a token whose teacher has no entry, or entries of
+ *         -infinity only.  An id >= V makes its token's KL NaN (and no gradient
+ *         of its own);
+ * kl      device fp32 [T]: KL_t, overwritten;
+ * loss_accum device fp32 [1] and stats device fp32 [2] are ACCUMULATED (+=):
+ *         stats = {tokens not masked that have a teacher, sum of their KL_t};
+ * dlogits device, type and row stride of logits, or NULL (no gradient): overwritten
+ *         in columns [0, V) of every row; may be `logits` itself.
+ * ws      device, >= rbp_workspace_bytes(RBP_OP_DISTILL, T, K, V).
+ * Errors: RBP_EINVAL (null pointers, T < 0, V < 1, K < 1, ld < V, B < 1, n_seq_total
+ *         < 1, an unknown type, temperature not positive and finite, scale not
+ *         finite, logits or dlogits not aligned to their type);
+ *         RBP_EUNSUPPORTED (K above 256, T above 2^31 - 1); RBP_EWORKSPACE.
+ */
+int policy_distill_fwd_bwd(const void* logits, int logits_type, int64_t ld,
+                           const int32_t* teacher_ids, const float* teacher_logits,
+                           const float* teacher_lse, const int32_t* seq_of_token,
+                           const int32_t* seq_len, int64_t T, int32_t V, int32_t K,
+                           int32_t B, int64_t n_seq_total, float temperature, float scale,
+                           float* kl, float* loss_accum, float* stats, void* dlogits,
+                           void* ws, size_t ws_bytes, void* stream);
 
 /* Workspace bytes an operation needs (see RBP_OP_*); 0 for an invalid op. */
 size_t rbp_workspace_bytes(int op, int64_t n, int32_t d, int32_t V);

@@ -37,6 +37,12 @@ RBP_OP_LOGPROB_BWD = 4
 RBP_OP_LOSS_SEQ = 5
 RBP_OP_FUSED = 6
 RBP_OP_NOTE_USE = 7
+RBP_OP_EMBED_BWD = 8
+RBP_OP_DISTILL = 9
+RBP_OP_VERIFY = 10
+
+RBP_BF16 = 0
+RBP_F32 = 1
 
 RBP_PHASE_START = 0
 RBP_PHASE_LOGITS = 1
@@ -52,7 +58,8 @@ EXPORTED = (
     "policy_loss_fwd_bwd", "policy_logprob_bwd", "rbp_workspace_bytes",
     "rbp_status_string", "rbp_last_error", "policy_loss_seq_fwd_bwd", "rb_asymre_coef",
     "policy_asymre_fwd_bwd", "policy_fused_fwd_bwd", "rb_push", "rb_note_use",
-    "rb_hist_accumulate", "rb_sample_gather_noalloc",
+    "rb_hist_accumulate", "rb_sample_gather_noalloc", "policy_embed_fwd", "policy_embed_bwd",
+    "policy_verify_drafts", "policy_distill_fwd_bwd",
 )
 
 
@@ -142,6 +149,13 @@ def load_library(path=LIB_PATH):
                             f32, vp]
     lib.rb_note_use.argtypes = [vp, i64, i64, i64, i64, vp, vp, vp, vp, sz, vp]
     lib.rb_hist_accumulate.argtypes = [vp, i64, i32, i32, vp, vp]
+    lib.policy_embed_fwd.argtypes = [vp, vp, vp, i64, i32, i32, f32, vp, vp]
+    lib.policy_embed_bwd.argtypes = [vp, ctypes.c_int, vp, vp, i64, i32, i32, f32, vp,
+                                     ctypes.c_int, vp, sz, vp]
+    lib.policy_verify_drafts.argtypes = [vp, vp, ctypes.c_int, i64, i64, vp, vp, vp, i32, i32, i32,
+                                         f32, vp, vp, vp, vp, sz, vp]
+    lib.policy_distill_fwd_bwd.argtypes = [vp, ctypes.c_int, i64, vp, vp, vp, vp, vp, i64, i32,
+                                           i32, i32, i64, f32, f32, vp, vp, vp, vp, vp, sz, vp]
     lib.rbp_workspace_bytes.argtypes = [ctypes.c_int, i64, i32, i32]
     lib.rbp_workspace_bytes.restype = sz
     lib.rbp_status_string.argtypes = [ctypes.c_int]
@@ -421,3 +435,44 @@ def rb_hist_accumulate(values, hist, lo=0, stream=None):
     st = (_N or _native()).hist_accumulate(values, hist, int(lo), stream)
     if st:
         _check("rb_hist_accumulate", st)
+
+
+def policy_embed_fwd(table, tokens, seq_of_token, out, scale=1.0, stream=None):
+    """out[t] = scale * table[tokens[t]]; seq_of_token (or None): negative entries mask."""
+    st = (_N or _native()).embed_fwd(table, tokens, seq_of_token, out, float(scale), stream)
+    if st:
+        _check("policy_embed_fwd", st)
+
+
+def policy_embed_bwd(dx, tokens, seq_of_token, dW, ws, scale=1.0, accumulate_dW=False,
+                     stream=None):
+    """dW[v] (+)= scale * the sum of dx[t] over the tokens v; dx bf16 or fp32, dW fp32."""
+    st = (_N or _native()).embed_bwd(dx, tokens, seq_of_token, dW, ws, float(scale),
+                                     1 if accumulate_dW else 0, stream)
+    if st:
+        _check("policy_embed_bwd", st)
+
+
+def policy_verify_drafts(logits, draft_logits, draft_tokens, n_draft, u, out_tokens, out_logp,
+                         n_out, ws, temperature=1.0, stream=None):
+    """logits [B, K + 1, V], draft_logits [B, K, V] or None, bf16 or fp32; rows may be
+    further apart than V (a slice of a padded vocabulary), evenly.  draft_tokens may be
+    None when K = 0, n_draft when every sequence has K drafts."""
+    st = (_N or _native()).verify_drafts(logits, draft_logits, draft_tokens, n_draft, u,
+                                         out_tokens, out_logp, n_out, ws, float(temperature),
+                                         stream)
+    if st:
+        _check("policy_verify_drafts", st)
+
+
+def policy_distill_fwd_bwd(logits, teacher_ids, teacher_logits, teacher_lse, seq_of_token,
+                           seq_len, n_seq_total, kl, loss_accum, stats, dlogits, ws,
+                           temperature=1.0, scale=1.0, stream=None):
+    """logits [T, V] bf16 or fp32, rows V or more apart; teacher_ids, teacher_logits [T, K];
+    dlogits None, logits itself, or a tensor of its dtype and strides."""
+    st = (_N or _native()).distill_fwd_bwd(logits, teacher_ids, teacher_logits, teacher_lse,
+                                           seq_of_token, seq_len, int(n_seq_total), kl,
+                                           loss_accum, stats, dlogits, ws, float(temperature),
+                                           float(scale), stream)
+    if st:
+        _check("policy_distill_fwd_bwd", st)

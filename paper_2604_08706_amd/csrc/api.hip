@@ -40,6 +40,9 @@ extern "C" size_t rbp_workspace_bytes(int op, int64_t n, int32_t d, int32_t V) {
     case RBP_OP_LOSS_SEQ: return rbp::loss_seq_ws(n);
     case RBP_OP_FUSED: return rbp::fused_ws(n, d, V);
     case RBP_OP_NOTE_USE: return rbp::note_use_ws(n);
+    case RBP_OP_EMBED_BWD: return rbp::embed_bwd_ws(n, d, V);
+    case RBP_OP_DISTILL: return rbp::distill_ws(n, d, V);
+    case RBP_OP_VERIFY: return rbp::verify_ws(n, d, V);
     default: return 0;
   }
 }

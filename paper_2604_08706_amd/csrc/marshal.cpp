@@ -135,6 +135,46 @@ void* stream(PyObject* o) {
   return p;
 }
 
+// Throws unless the tensor (None is passed over) lies on the current device,
+// whose stream the call uses.
+void here(PyObject* o, const char* name) {
+  if (o == Py_None) return;
+  const at::Tensor& t = tensor(o, name);
+  if (t.is_cuda() && t.device().index() != c10::hip::current_device())
+    raise(PyExc_ValueError, "%s is not on the current device", name);
+}
+
+// Logits [..., V] in bf16 or fp32 whose rows, over the leading dimensions, lie
+// evenly spaced in memory (a slice of a padded vocabulary is fine).
+struct Rows {
+  void* p;
+  int type;
+  int64_t ld;
+};
+Rows rows(PyObject* o, const char* name, int64_t dims) {
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda()) raise(PyExc_ValueError, "%s must be a device tensor", name);
+  here(o, name);
+  if (t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat)
+    raise(PyExc_TypeError, "%s must be torch.bfloat16 or torch.float32", name);
+  if (t.dim() != dims) raise(PyExc_ValueError, "%s has the wrong number of dimensions", name);
+  const int64_t V = t.size(dims - 1);
+  bool even = V <= 1 || t.stride(dims - 1) == 1;
+  int64_t ld = -1, n = 1;  // row stride, rows of the dimensions inside the present one
+  for (int64_t k = dims - 2; k >= 0; --k) {
+    if (t.size(k) > 1) {
+      if (ld < 0) ld = t.stride(k) / n;
+      even = even && t.stride(k) == ld * n;
+    }
+    n *= t.size(k);
+  }
+  if (ld < 0) ld = V;  // one row at most
+  if (n > 0 && (!even || ld < V))
+    raise(PyExc_ValueError, "%s must have contiguous rows, evenly spaced", name);
+  if (ld < V) ld = V;  // no rows
+  return {t.data_ptr(), t.scalar_type() == at::kFloat ? RBP_F32 : RBP_BF16, ld};
+}
+
 // The C struct inside a ctypes.Structure (of the class registered for it).
 struct StructView {
   Py_buffer b{};
@@ -445,6 +485,108 @@ PyObject* hist_accumulate(const Args& a) {  // values hist lo stream
   return run([&] { return rb_hist_accumulate(v, n, lo, (int32_t)bins, hist, s); });
 }
 
+PyObject* embed_fwd(const Args& a) {  // table tokens seq out scale stream
+  int64_t V, d;
+  sizes_2d(a[0], "table", V, d);
+  const int64_t T = numel_of(a[1], "tokens");
+  const uint16_t* table = bf16(a[0], "table", V * d);
+  const int32_t *tok = i32(a[1], "tokens", T), *seq = i32_or_null(a[2], "seq_of_token", T);
+  uint16_t* out = bf16(a[3], "out", T * d);
+  here(a[0], "table"), here(a[1], "tokens"), here(a[2], "seq_of_token"), here(a[3], "out");
+  const float scale = real(a[4]);
+  void* s = stream(a[5]);
+  return run(
+      [&] { return policy_embed_fwd(table, tok, seq, T, (int32_t)d, (int32_t)V, scale, out, s); });
+}
+
+PyObject* embed_bwd(const Args& a) {  // dx tokens seq dW ws scale accumulate stream
+  int64_t V, d;
+  sizes_2d(a[3], "dW", V, d);
+  const int64_t T = numel_of(a[1], "tokens");
+  const at::Tensor& x = tensor(a[0], "dx");
+  const bool wide = x.scalar_type() == at::kFloat;
+  const void* dx = wide ? (const void*)f32(a[0], "dx", T * d) : bf16(a[0], "dx", T * d);
+  const int32_t *tok = i32(a[1], "tokens", T), *seq = i32_or_null(a[2], "seq_of_token", T);
+  float* dW = f32(a[3], "dW", V * d);
+  const Workspace ws = workspace(a[4]);
+  here(a[0], "dx"), here(a[1], "tokens"), here(a[2], "seq_of_token"), here(a[3], "dW");
+  here(a[4], "ws");
+  const float scale = real(a[5]);
+  const int acc = (int)integer(a[6]);
+  void* s = stream(a[7]);
+  return run([&] {
+    return policy_embed_bwd(dx, wide ? RBP_F32 : RBP_BF16, tok, seq, T, (int32_t)d, (int32_t)V,
+                            scale, dW, acc, ws.p, ws.bytes, s);
+  });
+}
+
+// logits draft_logits draft_tokens n_draft u out_tokens out_logp n_out ws temperature stream
+PyObject* verify_drafts(const Args& a) {
+  const Rows z = rows(a[0], "logits", 3);
+  const int64_t B = size_of(a[0], "logits", 0), K = size_of(a[0], "logits", 1) - 1,
+                V = size_of(a[0], "logits", 2);
+  Rows q{nullptr, z.type, V};
+  if (a[1] != Py_None) {
+    q = rows(a[1], "draft_logits", 3);
+    if (q.type != z.type) raise(PyExc_TypeError, "%s must have the type of logits", "draft_logits");
+    if (size_of(a[1], "draft_logits", 0) != B || size_of(a[1], "draft_logits", 1) != K ||
+        size_of(a[1], "draft_logits", 2) != V)
+      raise(PyExc_ValueError, "%s must be [B, K, V]", "draft_logits");
+    if (K < 1) q.p = nullptr;  // nothing to read
+  }
+  const int64_t n = K < 0 ? 0 : B * K;
+  const int32_t *x = i32_or_null(a[2], "draft_tokens", n), *nd = i32_or_null(a[3], "n_draft", B);
+  const float* u = f32(a[4], "u", n + B);
+  int32_t* out = i32(a[5], "out_tokens", n + B);
+  float* lp = f32(a[6], "out_logp", n + B);
+  int32_t* n_out = i32(a[7], "n_out", B);
+  const Workspace ws = workspace(a[8]);
+  here(a[2], "draft_tokens"), here(a[3], "n_draft"), here(a[4], "u"), here(a[5], "out_tokens");
+  here(a[6], "out_logp"), here(a[7], "n_out"), here(a[8], "ws");
+  const float temp = real(a[9]);
+  void* s = stream(a[10]);
+  return run([&] {
+    return policy_verify_drafts(z.p, q.p, z.type, z.ld, q.ld, x, nd, u, (int32_t)B, (int32_t)K,
+                                (int32_t)V, temp, out, lp, n_out, ws.p, ws.bytes, s);
+  });
+}
+
+// logits ids teacher mass seq seq_len n_seq_total kl loss stats dlogits ws temperature scale stream
+PyObject* distill_fwd_bwd(const Args& a) {
+  const Rows z = rows(a[0], "logits", 2);
+  const int64_t T = size_of(a[0], "logits", 0), V = size_of(a[0], "logits", 1);
+  int64_t Ti, K;
+  sizes_2d(a[1], "teacher_ids", Ti, K);
+  if (Ti != T) raise(PyExc_ValueError, "%s must be [T, K]", "teacher_ids");
+  const int64_t B = numel_of(a[5], "seq_len");
+  const int32_t* ids = i32(a[1], "teacher_ids", T * K);
+  const float *lt = f32(a[2], "teacher_logits", T * K), *mass = f32_or_null(a[3], "teacher_lse", T);
+  const int32_t *seq = i32(a[4], "seq_of_token", T), *len = i32(a[5], "seq_len", B);
+  const int64_t n_seq = integer(a[6]);
+  float *kl = f32(a[7], "kl", T), *loss = f32(a[8], "loss_accum", 1),
+        *stats = f32(a[9], "stats", 2);
+  void* dz = nullptr;
+  if (a[10] != Py_None) {
+    const Rows g = rows(a[10], "dlogits", 2);
+    if (g.type != z.type) raise(PyExc_TypeError, "%s must have the type of logits", "dlogits");
+    if (size_of(a[10], "dlogits", 0) != T || size_of(a[10], "dlogits", 1) != V ||
+        (T > 1 && g.ld != z.ld))
+      raise(PyExc_ValueError, "%s must have the shape and strides of logits", "dlogits");
+    dz = g.p;
+  }
+  const Workspace ws = workspace(a[11]);
+  here(a[1], "teacher_ids"), here(a[2], "teacher_logits"), here(a[3], "teacher_lse");
+  here(a[4], "seq_of_token"), here(a[5], "seq_len"), here(a[7], "kl"), here(a[8], "loss_accum");
+  here(a[9], "stats"), here(a[11], "ws");
+  const float temp = real(a[12]), scale = real(a[13]);
+  void* s = stream(a[14]);
+  return run([&] {
+    return policy_distill_fwd_bwd(z.p, z.type, z.ld, ids, lt, mass, seq, len, T, (int32_t)V,
+                                  (int32_t)K, (int32_t)B, n_seq, temp, scale, kl, loss, stats, dz,
+                                  ws.p, ws.bytes, s);
+  });
+}
+
 #define RBP_ENTRY(name) \
   {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RBP_ENTRY(set_structs),
@@ -461,6 +603,10 @@ PyMethodDef methods[] = {RBP_ENTRY(set_structs),
                          RBP_ENTRY(push),
                          RBP_ENTRY(note_use),
                          RBP_ENTRY(hist_accumulate),
+                         RBP_ENTRY(embed_fwd),
+                         RBP_ENTRY(embed_bwd),
+                         RBP_ENTRY(verify_drafts),
+                         RBP_ENTRY(distill_fwd_bwd),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 

@@ -41,6 +41,9 @@ size_t loss_seq_ws(int64_t B);
 size_t logprob_bwd_ws(int64_t Tc, int32_t d, int32_t V);
 size_t fused_ws(int64_t Tc, int32_t d, int32_t V);
 size_t note_use_ws(int64_t capacity);
+size_t embed_bwd_ws(int64_t T, int32_t d, int32_t V);
+size_t distill_ws(int64_t T, int32_t K, int32_t V);
+size_t verify_ws(int64_t B, int32_t K, int32_t V);
 
 // The two products of the log-prob backward for one chunk of Tn tokens, from
 // dz^T (bf16 [round256(V)][ldGt], columns Tn..round256(Tn) zero):
