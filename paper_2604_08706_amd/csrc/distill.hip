@@ -5,7 +5,10 @@
 //   lse = log sum_v exp(y_v),  KL = sum_k p_k (log p_k - y_{id_k} + lse),
 //   dz_v = w / tau (P exp(y_v - lse) - sum_{k: id_k = v} p_k),  P = sum_k p_k,
 //   w = scale / (n_seq len_i),  loss += sum_t w_t KL_t.
-// Bound by HBM: each logit is read and its gradient written once.
+// Bound by HBM: each logit is read and its gradient written once.  A row of
+// 152064 bf16 logits (297 KB) fits the 512 KB of registers of a compute unit, so
+// one block reads it into registers, reduces it with a running reference and sum
+// as it arrives, and writes the gradient from there.
 
 #include "logits_epilogue.h"
 #include "rbp_internal.h"
@@ -13,17 +16,11 @@
 namespace {
 
 using rbp::lp::bf16_to_f32;
+using rbp::lp::exp2_hw;
 using rbp::lp::kLog2e;
+using rbp::lp::pack_bf16x2;
 
-constexpr int kThreads = 256;
 constexpr int kMaxK = 256;
-
-__device__ __forceinline__ float value(const float* p, int64_t i) { return p[i]; }
-__device__ __forceinline__ float value(const uint16_t* p, int64_t i) { return bf16_to_f32(p[i]); }
-__device__ __forceinline__ void put(float* p, int64_t i, float v) { p[i] = v; }
-__device__ __forceinline__ void put(uint16_t* p, int64_t i, float v) {
-  p[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
-}
 
 struct Args {
   int64_t ld;
@@ -35,86 +32,310 @@ struct Args {
   float *kl, *terms;      // terms: [T][2] loss term, 1 if the token counts
 };
 
-__device__ __forceinline__ float block_max(float v, float* s) {
-  v = rbp::lp::wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = s[0];
-  for (int w = 1; w < kThreads / 64; ++w) v = fmaxf(v, s[w]);
-  return v;
-}
-__device__ __forceinline__ float block_sum(float v, float* s) {
-  v = rbp::lp::wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.0f;
-  for (int w = 0; w < kThreads / 64; ++w) v += s[w];
-  return v;
+// A row of logits as 16-byte pieces: the pieces that lie whole and aligned in
+// it, and up to 2 (E - 1) elements before and behind them.
+template <class X>
+struct Row {
+  static constexpr int E = 16 / sizeof(X);  // elements per piece
+  int32_t head, pieces, V;
+  __device__ __forceinline__ Row(const X* row, int32_t V_) : V(V_) {
+    const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(X));
+    head = (E - off) % E;
+    if (head > V) head = V;
+    pieces = (V - head) / E;
+  }
+  __device__ __forceinline__ int32_t at(int32_t piece) const { return head + piece * E; }
+  // the loose element that thread tid takes, -1 for none
+  __device__ __forceinline__ int32_t loose(int tid) const {
+    const int32_t v = tid < head ? tid : pieces * E + tid;
+    return tid < 2 * E && v < V ? v : -1;
+  }
+  // the thread that takes element v
+  template <int kThreads>
+  __device__ __forceinline__ int owner(int32_t v) const {
+    if (v < head) return v;
+    const int32_t p = (v - head) / E;
+    return p < pieces ? p % kThreads : v - pieces * E;
+  }
+};
+
+__device__ __forceinline__ float value(float v) { return v; }
+__device__ __forceinline__ float value(uint16_t v) { return bf16_to_f32(v); }
+__device__ __forceinline__ void to(float& o, float v) { o = v; }
+__device__ __forceinline__ void to(uint16_t& o, float v) {
+  o = __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// A block per token: the teacher's entries one per thread, then two passes over
-// the logits.
-template <class X>
-__global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz, Args a) {
-  __shared__ float s[kThreads / 64], ps[kMaxK];
-  __shared__ int32_t is[kMaxK];
-  const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x;
-  const X* row = z + t * a.ld;
-  X* grad = dz == nullptr ? nullptr : dz + t * a.ld;
-  const int32_t sq = a.seq[t];
-  int32_t id = -1;
-  float l = -INFINITY;
-  if (sq >= 0 && tid < a.K) {
-    id = a.ids[t * a.K + tid];
-    if (id >= 0) l = a.lt[t * a.K + tid] * a.inv_tau;
+// A piece's elements, and back.
+__device__ __forceinline__ void unpack(const uint4& p, float (&x)[4]) {
+  x[0] = __uint_as_float(p.x), x[1] = __uint_as_float(p.y);
+  x[2] = __uint_as_float(p.z), x[3] = __uint_as_float(p.w);
+}
+__device__ __forceinline__ void unpack(const uint4& p, float (&x)[8]) {
+  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    x[2 * k] = __uint_as_float(w[k] << 16);
+    x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
   }
-  const bool nan = block_max(l != l ? 1.0f : 0.0f, s) > 0.0f;
-  const float lm = block_max(l, s);
-  if (sq < 0 || (lm == -INFINITY && !nan)) {
-    if (grad != nullptr)
-      for (int32_t v = tid; v < a.V; v += kThreads) put(grad, v, 0.0f);
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                    __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                    pack_bf16x2(x[6], x[7]));
+}
+
+// Running reference and sum of a thread: s = sum exp((z - m) inv_tau).  m follows
+// the largest logit only once that is kSlack (in powers of two) above it: sums
+// stay far from overflow, and rescaling is rare.
+constexpr float kSlack = 20.0f;
+struct Online {
+  float m = -INFINITY, s = 0.0f;
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N], float k2, float slack) {
+    float top = x[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) top = fmaxf(top, x[k]);
+    if (top > m + slack) {
+      s *= exp2_hw((m - top) * k2);
+      m = top;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;  // nothing but -inf so far
+    float e[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) e[k] = exp2_hw((x[k] - ref) * k2);
+#pragma unroll
+    for (int w = N / 2; w >= 1; w /= 2)
+#pragma unroll
+      for (int k = 0; k < w; ++k) e[k] += e[k + w];
+    s += e[0];
+  }
+};
+
+// A block per token.  Each thread keeps kHold pieces of the row in registers, so
+// that a row of up to kThreads * kHold pieces is read from memory once; the
+// pieces beyond them are read again for the gradient.  The first wave prepares
+// the teacher's entries while the row arrives.  An element that the teacher
+// names gets its gradient a second time, by the thread that wrote it the first
+// (a thread's stores to one address stay in order), so that the loop over the
+// row looks for nothing.
+template <class X, int kThreads, int kHold, bool kGrad>
+__global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz, Args a) {
+  constexpr int E = Row<X>::E, kWaves = kThreads / 64;
+  __shared__ float m_s[kWaves], s_s[kWaves];
+  __shared__ float mass_s;                       // P
+  __shared__ int32_t any_s;
+  __shared__ int32_t id_s[kMaxK];
+  __shared__ float p_s[kMaxK], z_s[kMaxK], e_s[kMaxK], dup_s[kMaxK];
+  const int64_t t = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const X* row = z + t * a.ld;
+  X* grad = kGrad ? dz + t * a.ld : nullptr;
+  const Row<X> r(row, a.V);
+  const bool vec = kGrad && ((reinterpret_cast<uintptr_t>(row) ^
+                              reinterpret_cast<uintptr_t>(grad)) & 15) == 0;
+  const int32_t loose = r.loose(tid);
+  const int32_t sq = a.seq[t];
+  auto put = [&](int32_t piece, const uint4& v) {
+    X* to_ = grad + r.at(piece);
+    if (vec) {
+      *reinterpret_cast<uint4*>(to_) = v;
+    } else {
+      X e[E];
+      __builtin_memcpy(e, &v, 16);
+#pragma unroll
+      for (int k = 0; k < E; ++k) to_[k] = e[k];
+    }
+  };
+  auto zeros = [&] {  // no teacher, or masked
     if (tid == 0) {
       a.kl[t] = 0.0f;
       a.terms[2 * t] = 0.0f;
       a.terms[2 * t + 1] = 0.0f;
     }
-    return;
+    if constexpr (kGrad) {
+      for (int32_t c = tid; c < r.pieces; c += kThreads) put(c, make_uint4(0u, 0u, 0u, 0u));
+      if (loose >= 0) grad[loose] = X(0);
+    }
+  };
+  if (sq < 0) return zeros();
+
+  uint4 hold[kHold > 0 ? kHold : 1];
+#pragma unroll
+  for (int i = 0; i < kHold; ++i) {
+    const int32_t c = i * kThreads + tid;
+    if (c < r.pieces) hold[i] = *reinterpret_cast<const uint4*>(row + r.at(c));
   }
-  const float mass =
-      a.mass != nullptr ? a.mass[t] : lm + logf(block_sum(id >= 0 ? expf(l - lm) : 0.0f, s));
-  const float logp = l - mass, p = id >= 0 ? expf(logp) : 0.0f;
-  const float P = block_sum(p, s);
-  float m = -INFINITY;
-  for (int32_t v = tid; v < a.V; v += kThreads) m = fmaxf(m, value(row, v));
-  m = block_max(m, s);
-  float sum = 0.0f;
-  for (int32_t v = tid; v < a.V; v += kThreads) sum += expf((value(row, v) - m) * a.inv_tau);
-  sum = block_sum(sum, s);
-  const float lse = m * a.inv_tau + logf(sum);
-  float term = 0.0f;
-  if (p != 0.0f) term = id < a.V ? p * (logp - value(row, id) * a.inv_tau + lse) : NAN;
-  const float kl = block_sum(term, s);
-  const float w = a.weight / (float)a.len[sq];
-  if (tid == 0) {
-    a.kl[t] = kl;
-    a.terms[2 * t] = w * kl;
-    a.terms[2 * t + 1] = 1.0f;
+  const float edge = loose >= 0 ? value(row[loose]) : -INFINITY;
+
+  if (wave == 0) {
+    constexpr int kPer = kMaxK / 64;
+    int32_t id[kPer];
+    float l[kPer], p[kPer];
+    float top = -INFINITY, nan = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int k = j * 64 + lane;
+      id[j] = -1;
+      l[j] = -INFINITY;
+      if (k < a.K) {
+        id[j] = a.ids[t * a.K + k];
+        if (id[j] >= 0) l[j] = a.lt[t * a.K + k] * a.inv_tau;
+      }
+      top = fmaxf(top, l[j]);
+      if (l[j] != l[j]) nan = 1.0f;
+    }
+    top = rbp::lp::wave_max(top);
+    nan = rbp::lp::wave_max(nan);
+    float mass = 0.0f, P = 0.0f;
+    if (a.mass != nullptr) {
+      mass = a.mass[t];
+    } else {
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) sum += id[j] >= 0 ? expf(l[j] - top) : 0.0f;
+      mass = top + logf(rbp::lp::wave_sum(sum));
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int k = j * 64 + lane;
+      const float logp = l[j] - mass;
+      p[j] = id[j] >= 0 ? expf(logp) : 0.0f;
+      P += p[j];
+      if (k < a.K) {
+        const float zk = id[j] >= 0 && id[j] < a.V ? value(row[id[j]]) : NAN;
+        id_s[k] = id[j];
+        p_s[k] = p[j];
+        z_s[k] = zk;
+        e_s[k] = logp - zk * a.inv_tau;
+      }
+    }
+    P = rbp::lp::wave_sum(P);
+    if (lane == 0) {
+      mass_s = P;
+      any_s = top > -INFINITY || nan > 0.0f;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (kGrad) {  // an id that occurs twice: all of its mass
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const int k = j * 64 + lane;
+        if (j * 64 >= a.K) break;
+        float all = 0.0f;
+        for (int i = 0; i < a.K; ++i) all += id_s[i] == id[j] ? p_s[i] : 0.0f;
+        if (k < a.K) dup_s[k] = all;
+      }
+    }
   }
-  if (grad == nullptr) return;
-  if (tid < a.K) {
-    ps[tid] = p;
-    is[tid] = id;
+
+  const float k2 = a.inv_tau * kLog2e, slack = fminf(kSlack / k2, 1e30f);
+  Online o;
+#pragma unroll
+  for (int i = 0; i < kHold; ++i) {
+    if (i * kThreads + tid < r.pieces) {
+      float x[E];
+      unpack(hold[i], x);
+      o.add(x, k2, slack);
+    }
+  }
+  constexpr int kBatch = 4;  // loads in flight
+  int32_t c = kHold * kThreads + tid;
+  for (; c + (kBatch - 1) * kThreads < r.pieces; c += kBatch * kThreads) {
+    uint4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      v[i] = *reinterpret_cast<const uint4*>(row + r.at(c + i * kThreads));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      float x[E];
+      unpack(v[i], x);
+      o.add(x, k2, slack);
+    }
+  }
+  for (; c < r.pieces; c += kThreads) {
+    float x[E];
+    unpack(*reinterpret_cast<const uint4*>(row + r.at(c)), x);
+    o.add(x, k2, slack);
+  }
+  const float last[1] = {edge};
+  o.add(last, k2, slack);
+
+  // the row's reference (not below its threads') and sum
+  auto rebase = [&](float s, float from, float onto) {
+    return from == -INFINITY ? s : s * exp2_hw((from - onto) * k2);
+  };
+  float M = rbp::lp::wave_max(o.m);
+  float S = rbp::lp::wave_sum(rebase(o.s, o.m, M));
+  if (lane == 0) {
+    m_s[wave] = M;
+    s_s[wave] = S;
   }
   __syncthreads();
-  const float c = w * a.inv_tau, f = c * P / sum;
-  for (int32_t v = tid; v < a.V; v += kThreads) {
-    float g = f * expf((value(row, v) - m) * a.inv_tau);
-    for (int k = 0; k < a.K; ++k)
-      if (is[k] == v) g -= c * ps[k];
-    put(grad, v, g);
+  if constexpr (kWaves > 1) {
+    M = m_s[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, m_s[w]);
+    S = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) S += rebase(s_s[w], m_s[w], M);
+  }
+  if (!any_s) return zeros();
+  const float w = a.weight / (float)a.len[sq];
+  if (wave == 0) {
+    const float lse = M * a.inv_tau + logf(S);
+    float kl = 0.0f;
+    for (int k = lane; k < a.K; k += 64)
+      if (p_s[k] != 0.0f) kl += p_s[k] * (e_s[k] + lse);
+    kl = rbp::lp::wave_sum(kl);
+    if (lane == 0) {
+      a.kl[t] = kl;
+      a.terms[2 * t] = w * kl;
+      a.terms[2 * t + 1] = 1.0f;
+    }
+  }
+  if constexpr (kGrad) {
+    const float cw = w * a.inv_tau, f = cw * mass_s / S;
+    auto gradient = [&](const uint4& v) {
+      float x[E];
+      unpack(v, x);
+#pragma unroll
+      for (int k = 0; k < E; ++k) x[k] = f * exp2_hw((x[k] - M) * k2);
+      return pack(x);
+    };
+#pragma unroll
+    for (int i = 0; i < kHold; ++i) {
+      const int32_t p = i * kThreads + tid;
+      if (p < r.pieces) put(p, gradient(hold[i]));
+    }
+    int32_t p = kHold * kThreads + tid;
+    for (; p + (kBatch - 1) * kThreads < r.pieces; p += kBatch * kThreads) {
+      uint4 v[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        v[i] = *reinterpret_cast<const uint4*>(row + r.at(p + i * kThreads));
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) put(p + i * kThreads, gradient(v[i]));
+    }
+    for (; p < r.pieces; p += kThreads)
+      put(p, gradient(*reinterpret_cast<const uint4*>(row + r.at(p))));
+    if (loose >= 0) to(grad[loose], f * exp2_hw((edge - M) * k2));
+    for (int k0 = 0; k0 < a.K; k0 += 64) {
+      const int32_t id = k0 + lane < a.K ? id_s[k0 + lane] : -1;
+      const int own = id >= 0 && id < a.V ? r.template owner<kThreads>(id) : -1;
+      uint64_t mine = __ballot(own >= 0 && (own >> 6) == wave);
+      while (mine != 0) {
+        const int j = __builtin_ctzll(mine);
+        mine &= mine - 1;
+        if (lane == (__shfl(own, j, 64) & 63)) {
+          const int k = k0 + j;
+          to(grad[id_s[k]], f * exp2_hw((z_s[k] - M) * k2) - cw * dup_s[k]);
+        }
+      }
+    }
   }
 }
 
@@ -141,6 +362,35 @@ __global__ void __launch_bounds__(1024) distill_sum_kernel(const float* __restri
   for (int w = 0; w < 16; ++w) sum += s[threadIdx.x][w];
   float* to = threadIdx.x == 0 ? loss_accum : stats + (threadIdx.x - 1);
   *to = (float)((double)*to + sum);
+}
+
+// Threads and pieces held per thread by the row's length: small rows on few
+// threads, the largest on 1024 with as many pieces as their registers hold.
+template <class X>
+void launch_rows(const X* z, X* dz, int64_t T, const Args& a, hipStream_t s) {
+  const int64_t pieces = a.V / Row<X>::E;
+  auto go = [&](auto threads, auto hold) {
+    constexpr int kThreads = decltype(threads)::value, kHold = decltype(hold)::value;
+    if (dz == nullptr)
+      hipLaunchKernelGGL((distill_row_kernel<X, kThreads, 0, false>), dim3((unsigned)T),
+                         dim3(kThreads), 0, s, z, dz, a);
+    else
+      hipLaunchKernelGGL((distill_row_kernel<X, kThreads, kHold, true>), dim3((unsigned)T),
+                         dim3(kThreads), 0, s, z, dz, a);
+  };
+  using std::integral_constant;
+  if (pieces <= 64 * 4)
+    go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (pieces <= 256 * 4)
+    go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (pieces <= 256 * 8)
+    go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  else if (pieces <= 512 * 8)
+    go(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+  else if (pieces <= 1024 * 8)
+    go(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+  else
+    go(integral_constant<int, 1024>{}, integral_constant<int, 20>{});
 }
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -185,11 +435,9 @@ extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64
   const Args a{ld, teacher_ids, teacher_logits, teacher_lse, seq_of_token, seq_len, V, K,
                1.0f / temperature, (float)((double)scale / (double)n_seq_total), kl, terms};
   if (logits_type == RBP_F32)
-    hipLaunchKernelGGL(distill_row_kernel<float>, dim3((unsigned)T), dim3(kThreads), 0, s,
-                       static_cast<const float*>(logits), static_cast<float*>(dlogits), a);
+    launch_rows(static_cast<const float*>(logits), static_cast<float*>(dlogits), T, a, s);
   else
-    hipLaunchKernelGGL(distill_row_kernel<uint16_t>, dim3((unsigned)T), dim3(kThreads), 0, s,
-                       static_cast<const uint16_t*>(logits), static_cast<uint16_t*>(dlogits), a);
+    launch_rows(static_cast<const uint16_t*>(logits), static_cast<uint16_t*>(dlogits), T, a, s);
   hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, terms, kl, T, loss_accum,
                      stats);
   RBP_CHECK_LAUNCH("policy_distill_fwd_bwd");
