@@ -50,13 +50,6 @@ struct Row {
     const int32_t v = tid < head ? tid : pieces * E + tid;
     return tid < 2 * E && v < V ? v : -1;
   }
-  // the thread that takes element v
-  template <int kThreads>
-  __device__ __forceinline__ int owner(int32_t v) const {
-    if (v < head) return v;
-    const int32_t p = (v - head) / E;
-    return p < pieces ? p % kThreads : v - pieces * E;
-  }
 };
 
 __device__ __forceinline__ float value(float v) { return v; }
@@ -119,17 +112,17 @@ struct Online {
 // that a row of up to kThreads * kHold pieces is read from memory once; the
 // pieces beyond them are read again for the gradient.  The first wave prepares
 // the teacher's entries while the row arrives.  An element that the teacher
-// names gets its gradient a second time, by the thread that wrote it the first
-// (a thread's stores to one address stay in order), so that the loop over the
-// row looks for nothing.
-template <class X, int kThreads, int kHold, bool kGrad>
+// names gets its gradient a second time, behind a barrier, so that the loop over
+// the row looks for nothing.
+template <class X, int kThreads, int kHold, bool kGrad, bool kBypass>
 __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz, Args a) {
   constexpr int E = Row<X>::E, kWaves = kThreads / 64;
   __shared__ float m_s[kWaves], s_s[kWaves];
   __shared__ float mass_s;                       // P
   __shared__ int32_t any_s;
-  __shared__ int32_t id_s[kMaxK];
-  __shared__ float p_s[kMaxK], z_s[kMaxK], e_s[kMaxK], dup_s[kMaxK];
+  __shared__ __attribute__((aligned(16))) int32_t id_s[kMaxK];
+  __shared__ __attribute__((aligned(16))) float p_s[kMaxK];
+  __shared__ float z_s[kMaxK], e_s[kMaxK];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const X* row = z + t * a.ld;
@@ -141,7 +134,10 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
   const int32_t sq = a.seq[t];
   auto put = [&](int32_t piece, const uint4& v) {
     X* to_ = grad + r.at(piece);
-    if (vec) {
+    if (vec && kBypass) {
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(to_));
+    } else if (vec) {
       *reinterpret_cast<uint4*>(to_) = v;
     } else {
       X e[E];
@@ -205,7 +201,9 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
       const float logp = l[j] - mass;
       p[j] = id[j] >= 0 ? expf(logp) : 0.0f;
       P += p[j];
-      if (k < a.K) {
+      if (k >= a.K) {  // up to a whole quarter of entries
+        if (k < ((a.K + 3) & ~3)) id_s[k] = -1, p_s[k] = 0.0f;
+      } else {
         const float zk = id[j] >= 0 && id[j] < a.V ? value(row[id[j]]) : NAN;
         id_s[k] = id[j];
         p_s[k] = p[j];
@@ -217,18 +215,6 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
     if (lane == 0) {
       mass_s = P;
       any_s = top > -INFINITY || nan > 0.0f;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if constexpr (kGrad) {  // an id that occurs twice: all of its mass
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const int k = j * 64 + lane;
-        if (j * 64 >= a.K) break;
-        float all = 0.0f;
-        for (int i = 0; i < a.K; ++i) all += id_s[i] == id[j] ? p_s[i] : 0.0f;
-        if (k < a.K) dup_s[k] = all;
-      }
     }
   }
 
@@ -306,35 +292,42 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
       for (int k = 0; k < E; ++k) x[k] = f * exp2_hw((x[k] - M) * k2);
       return pack(x);
     };
+    // the pieces that are read again, latest first
+    if (kHold * kThreads + tid < r.pieces) {
+      int32_t p = kHold * kThreads + tid;
+      p += (r.pieces - 1 - p) / kThreads * kThreads;
+      for (; p - (kBatch - 1) * kThreads >= kHold * kThreads; p -= kBatch * kThreads) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          v[i] = *reinterpret_cast<const uint4*>(row + r.at(p - i * kThreads));
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) put(p - i * kThreads, gradient(v[i]));
+      }
+      for (; p >= kHold * kThreads; p -= kThreads)
+        put(p, gradient(*reinterpret_cast<const uint4*>(row + r.at(p))));
+    }
 #pragma unroll
     for (int i = 0; i < kHold; ++i) {
       const int32_t p = i * kThreads + tid;
       if (p < r.pieces) put(p, gradient(hold[i]));
     }
-    int32_t p = kHold * kThreads + tid;
-    for (; p + (kBatch - 1) * kThreads < r.pieces; p += kBatch * kThreads) {
-      uint4 v[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        v[i] = *reinterpret_cast<const uint4*>(row + r.at(p + i * kThreads));
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) put(p + i * kThreads, gradient(v[i]));
-    }
-    for (; p < r.pieces; p += kThreads)
-      put(p, gradient(*reinterpret_cast<const uint4*>(row + r.at(p))));
     if (loose >= 0) to(grad[loose], f * exp2_hw((edge - M) * k2));
-    for (int k0 = 0; k0 < a.K; k0 += 64) {
-      const int32_t id = k0 + lane < a.K ? id_s[k0 + lane] : -1;
-      const int own = id >= 0 && id < a.V ? r.template owner<kThreads>(id) : -1;
-      uint64_t mine = __ballot(own >= 0 && (own >> 6) == wave);
-      while (mine != 0) {
-        const int j = __builtin_ctzll(mine);
-        mine &= mine - 1;
-        if (lane == (__shfl(own, j, 64) & 63)) {
-          const int k = k0 + j;
-          to(grad[id_s[k]], f * exp2_hw((z_s[k] - M) * k2) - cw * dup_s[k]);
-        }
+    // the named elements again, once the row's stores are ordered before; an id
+    // that occurs twice has all of its mass, and the same value is stored twice
+    __syncthreads();
+    for (int k = tid; k < a.K; k += kThreads) {
+      const int32_t id = id_s[k];
+      if (id < 0 || id >= a.V) continue;
+      float all = 0.0f;
+#pragma unroll 2
+      for (int i = 0; i < a.K; i += 4) {
+        const int4 o = *reinterpret_cast<const int4*>(id_s + i);
+        const float4 q = *reinterpret_cast<const float4*>(p_s + i);
+        all += (o.x == id ? q.x : 0.0f) + (o.y == id ? q.y : 0.0f) + (o.z == id ? q.z : 0.0f) +
+               (o.w == id ? q.w : 0.0f);
       }
+      to(grad[id], f * exp2_hw((z_s[k] - M) * k2) - cw * all);
     }
   }
 }
@@ -369,14 +362,17 @@ __global__ void __launch_bounds__(1024) distill_sum_kernel(const float* __restri
 template <class X>
 void launch_rows(const X* z, X* dz, int64_t T, const Args& a, hipStream_t s) {
   const int64_t pieces = a.V / Row<X>::E;
+  // Stores past the caches where part of the row is read twice (the gradient must
+  // not push it out: 1301 x 151936 fp32 429 -> 329 us) and for passes of less than
+  // 3/4 GiB (512 x 151936 bf16 84 -> 73 us, 8192 x 12000 91 -> 89); beyond, cached
+  // stores are faster (16384 x 152064 1962 against 2024 us, 5000 612 / 635).
+  const bool bypass = pieces > 1024 * 20 || T * a.ld * (int64_t)sizeof(X) < (3ll << 28);
   auto go = [&](auto threads, auto hold) {
     constexpr int kThreads = decltype(threads)::value, kHold = decltype(hold)::value;
-    if (dz == nullptr)
-      hipLaunchKernelGGL((distill_row_kernel<X, kThreads, 0, false>), dim3((unsigned)T),
-                         dim3(kThreads), 0, s, z, dz, a);
-    else
-      hipLaunchKernelGGL((distill_row_kernel<X, kThreads, kHold, true>), dim3((unsigned)T),
-                         dim3(kThreads), 0, s, z, dz, a);
+    auto kernel = dz == nullptr ? distill_row_kernel<X, kThreads, 0, false, false>
+                  : bypass      ? distill_row_kernel<X, kThreads, kHold, true, true>
+                                : distill_row_kernel<X, kThreads, kHold, true, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(kThreads), 0, s, z, dz, a);
   };
   using std::integral_constant;
   if (pieces <= 64 * 4)
