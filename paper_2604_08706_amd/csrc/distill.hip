@@ -108,6 +108,81 @@ struct Online {
   }
 };
 
+// The teacher's entries of a token, by one wave: entry k goes to id[k], p[k] (its
+// probability), y[k] (the policy's logit there) and e[k] = log p_k - y_k / tau;
+// up to a whole quarter of entries is filled with absent ones.
+struct Teacher {
+  float P;   // sum of p
+  double A;  // sum of p e: KL = A + P lse
+  bool any;  // an entry of some mass (or a NaN)
+};
+template <class X>
+__device__ __forceinline__ Teacher teacher_entries(const Args& a, int64_t t, const X* row,
+                                                   int lane, int32_t* id_s, float* p_s,
+                                                   float* z_s, float* e_s) {
+  constexpr int kPer = kMaxK / 64;
+  int32_t id[kPer];
+  float l[kPer];
+  float top = -INFINITY, nan = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int k = j * 64 + lane;
+    id[j] = -1;
+    l[j] = -INFINITY;
+    if (k < a.K) {
+      id[j] = a.ids[t * a.K + k];
+      if (id[j] >= 0) l[j] = a.lt[t * a.K + k] * a.inv_tau;
+    }
+    top = fmaxf(top, l[j]);
+    if (l[j] != l[j]) nan = 1.0f;
+  }
+  top = rbp::lp::wave_max(top);
+  nan = rbp::lp::wave_max(nan);
+  float mass = 0.0f, P = 0.0f;
+  if (a.mass != nullptr) {
+    mass = a.mass[t];
+  } else {
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) sum += id[j] >= 0 ? expf(l[j] - top) : 0.0f;
+    mass = top + logf(rbp::lp::wave_sum(sum));
+  }
+  double A = 0.0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int k = j * 64 + lane;
+    const float logp = l[j] - mass, p = id[j] >= 0 ? expf(logp) : 0.0f;
+    P += p;
+    if (k >= a.K) {
+      if (k < ((a.K + 3) & ~3)) id_s[k] = -1, p_s[k] = 0.0f;
+    } else {
+      const float zk = id[j] >= 0 && id[j] < a.V ? value(row[id[j]]) : NAN;
+      const float e = logp - zk * a.inv_tau;
+      id_s[k] = id[j];
+      p_s[k] = p;
+      z_s[k] = zk;
+      e_s[k] = e;
+      if (p != 0.0f) A += (double)p * (double)e;
+    }
+  }
+  for (int off = 32; off >= 1; off >>= 1) A += __shfl_xor(A, off, 64);
+  return {rbp::lp::wave_sum(P), A, top > -INFINITY || nan > 0.0f};
+}
+
+// The mass of an id over all entries that name it.
+__device__ __forceinline__ float mass_of(int32_t id, const int32_t* id_s, const float* p_s,
+                                         int32_t K) {
+  float all = 0.0f;
+#pragma unroll 2
+  for (int i = 0; i < K; i += 4) {
+    const int4 o = *reinterpret_cast<const int4*>(id_s + i);
+    const float4 q = *reinterpret_cast<const float4*>(p_s + i);
+    all += (o.x == id ? q.x : 0.0f) + (o.y == id ? q.y : 0.0f) + (o.z == id ? q.z : 0.0f) +
+           (o.w == id ? q.w : 0.0f);
+  }
+  return all;
+}
+
 // A block per token.  Each thread keeps kHold pieces of the row in registers, so
 // that a row of up to kThreads * kHold pieces is read from memory once; the
 // pieces beyond them are read again for the gradient.  The first wave prepares
@@ -168,53 +243,10 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
   const float edge = loose >= 0 ? value(row[loose]) : -INFINITY;
 
   if (wave == 0) {
-    constexpr int kPer = kMaxK / 64;
-    int32_t id[kPer];
-    float l[kPer], p[kPer];
-    float top = -INFINITY, nan = 0.0f;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int k = j * 64 + lane;
-      id[j] = -1;
-      l[j] = -INFINITY;
-      if (k < a.K) {
-        id[j] = a.ids[t * a.K + k];
-        if (id[j] >= 0) l[j] = a.lt[t * a.K + k] * a.inv_tau;
-      }
-      top = fmaxf(top, l[j]);
-      if (l[j] != l[j]) nan = 1.0f;
-    }
-    top = rbp::lp::wave_max(top);
-    nan = rbp::lp::wave_max(nan);
-    float mass = 0.0f, P = 0.0f;
-    if (a.mass != nullptr) {
-      mass = a.mass[t];
-    } else {
-      float sum = 0.0f;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) sum += id[j] >= 0 ? expf(l[j] - top) : 0.0f;
-      mass = top + logf(rbp::lp::wave_sum(sum));
-    }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int k = j * 64 + lane;
-      const float logp = l[j] - mass;
-      p[j] = id[j] >= 0 ? expf(logp) : 0.0f;
-      P += p[j];
-      if (k >= a.K) {  // up to a whole quarter of entries
-        if (k < ((a.K + 3) & ~3)) id_s[k] = -1, p_s[k] = 0.0f;
-      } else {
-        const float zk = id[j] >= 0 && id[j] < a.V ? value(row[id[j]]) : NAN;
-        id_s[k] = id[j];
-        p_s[k] = p[j];
-        z_s[k] = zk;
-        e_s[k] = logp - zk * a.inv_tau;
-      }
-    }
-    P = rbp::lp::wave_sum(P);
+    const Teacher te = teacher_entries(a, t, row, lane, id_s, p_s, z_s, e_s);
     if (lane == 0) {
-      mass_s = P;
-      any_s = top > -INFINITY || nan > 0.0f;
+      mass_s = te.P;
+      any_s = te.any;
     }
   }
 
@@ -319,17 +351,199 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
     for (int k = tid; k < a.K; k += kThreads) {
       const int32_t id = id_s[k];
       if (id < 0 || id >= a.V) continue;
-      float all = 0.0f;
-#pragma unroll 2
-      for (int i = 0; i < a.K; i += 4) {
-        const int4 o = *reinterpret_cast<const int4*>(id_s + i);
-        const float4 q = *reinterpret_cast<const float4*>(p_s + i);
-        all += (o.x == id ? q.x : 0.0f) + (o.y == id ? q.y : 0.0f) + (o.z == id ? q.z : 0.0f) +
-               (o.w == id ? q.w : 0.0f);
-      }
-      to(grad[id], f * exp2_hw((z_s[k] - M) * k2) - cw * all);
+      to(grad[id], f * exp2_hw((z_s[k] - M) * k2) - cw * mass_of(id, id_s, p_s, a.K));
     }
   }
+}
+
+// ---- few rows -------------------------------------------------------------------
+
+// With few rows (row_parts), `parts` blocks (a power of two, up to 64)
+// share a row: the first launch leaves each part's reference and sum, and what
+// the teacher says of the row; the second joins them in every block, writes the
+// gradient of the block's part, and in one more block the KLs and their sums.
+constexpr int kPartThreads = 256;
+struct PartsWs {
+  float2* stats;  // [T][parts] reference, sum
+  double* A;      // [T]
+  float2* row;    // [T] P, 1 if the row counts
+  float* p;       // [T][K]
+  int parts;
+};
+
+// (M, S) of a row from its parts, lane j of `parts` lanes holding part j.
+__device__ __forceinline__ float2 join(float2 part, int parts, float k2) {
+  float M = part.x;
+  for (int off = parts >> 1; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+  float S = part.x == -INFINITY ? part.y : part.y * exp2_hw((part.x - M) * k2);
+  for (int off = parts >> 1; off >= 1; off >>= 1) S += __shfl_xor(S, off, 64);
+  return make_float2(M, S);
+}
+
+template <class X>
+__global__ void __launch_bounds__(kPartThreads) distill_part_kernel(const X* __restrict__ z,
+                                                                    Args a, PartsWs w) {
+  constexpr int E = Row<X>::E, kWaves = kPartThreads / 64, kBatch = 4;
+  __shared__ float2 s[kWaves];
+  __shared__ int32_t id_s[kMaxK];
+  __shared__ float p_s[kMaxK], z_s[kMaxK], e_s[kMaxK];
+  const int64_t t = blockIdx.x / w.parts;
+  const int part = blockIdx.x % w.parts;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (a.seq[t] < 0) return;
+  const X* row = z + t * a.ld;
+  const Row<X> r(row, a.V);
+  const int32_t end = (int32_t)((int64_t)r.pieces * (part + 1) / w.parts);
+  int32_t c = (int32_t)((int64_t)r.pieces * part / w.parts) + tid;
+  const float k2 = a.inv_tau * kLog2e, slack = fminf(kSlack / k2, 1e30f);
+  Online o;
+  const int32_t loose = part == 0 ? r.loose(tid) : -1;
+  const float edge[1] = {loose >= 0 ? value(row[loose]) : -INFINITY};
+  for (; c < end; c += kBatch * kPartThreads) {
+    uint4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * kPartThreads < end)
+        v[i] = *reinterpret_cast<const uint4*>(row + r.at(c + i * kPartThreads));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * kPartThreads < end) {
+        float x[E];
+        unpack(v[i], x);
+        o.add(x, k2, slack);
+      }
+  }
+  o.add(edge, k2, slack);
+  const float2 mine = join(make_float2(o.m, o.s), 64, k2);
+  if (lane == 0) s[wave] = mine;
+  if (part == 0 && wave == kWaves - 1) {
+    const Teacher te = teacher_entries(a, t, row, lane, id_s, p_s, z_s, e_s);
+    for (int k = lane; k < a.K; k += 64) w.p[t * a.K + k] = p_s[k];
+    if (lane == 0) {
+      w.A[t] = te.A;
+      w.row[t] = make_float2(te.P, te.any ? 1.0f : 0.0f);
+    }
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const float2 all = join(lane < kWaves ? s[lane] : make_float2(-INFINITY, 0.0f), kWaves, k2);
+    if (lane == 0) w.stats[t * w.parts + part] = all;
+  }
+}
+
+template <class X>
+__global__ void __launch_bounds__(kPartThreads) distill_join_kernel(const X* z, X* dz, Args a,
+                                                                    PartsWs w, int64_t T,
+                                                                    float* loss_accum,
+                                                                    float* stats) {
+  constexpr int E = Row<X>::E, kBatch = 4;
+  __shared__ __attribute__((aligned(16))) int32_t id_s[kMaxK];
+  __shared__ __attribute__((aligned(16))) float p_s[kMaxK];
+  __shared__ float z_s[kMaxK];
+  __shared__ double sum_s[3][kPartThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float k2 = a.inv_tau * kLog2e;
+  if (blockIdx.x == 0) {  // KL of the rows and the sums over them
+    double v[3] = {0.0, 0.0, 0.0};
+    const int64_t n = T * w.parts;
+    for (int64_t i0 = 0; i0 < n; i0 += kPartThreads) {
+      const int64_t i = i0 + tid, t = i / w.parts;
+      const bool in = i < n, counts = in && a.seq[t] >= 0 && w.row[t].y > 0.0f;
+      const float2 all = join(counts ? w.stats[i] : make_float2(-INFINITY, 0.0f), w.parts, k2);
+      if (!in || i % w.parts != 0) continue;
+      float kl = 0.0f;
+      if (counts) {
+        kl = (float)(w.A[t] + (double)w.row[t].x *
+                                  ((double)(all.x * a.inv_tau) + (double)logf(all.y)));
+        v[0] += a.weight / (float)a.len[a.seq[t]] * kl;
+        v[1] += 1.0;
+        v[2] += kl;
+      }
+      a.kl[t] = kl;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      for (int off = 32; off >= 1; off >>= 1) v[k] += __shfl_xor(v[k], off, 64);
+      if (lane == 0) sum_s[k][wave] = v[k];
+    }
+    __syncthreads();
+    if (tid >= 3) return;
+    double sum = 0.0;
+    for (int q = 0; q < kPartThreads / 64; ++q) sum += sum_s[tid][q];
+    float* to_ = tid == 0 ? loss_accum : stats + (tid - 1);
+    *to_ = (float)((double)*to_ + sum);
+    return;
+  }
+  const int64_t t = (blockIdx.x - 1) / w.parts;
+  const int part = (blockIdx.x - 1) % w.parts;
+  const X* row = z + t * a.ld;
+  X* grad = dz + t * a.ld;
+  const Row<X> r(row, a.V);
+  const bool vec =
+      ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0;
+  const int32_t begin = (int32_t)((int64_t)r.pieces * part / w.parts),
+                end = (int32_t)((int64_t)r.pieces * (part + 1) / w.parts);
+  const int32_t loose = part == 0 ? r.loose(tid) : -1;
+  const int32_t sq = a.seq[t];
+  const bool counts = sq >= 0 && w.row[t].y > 0.0f;
+  auto put = [&](int32_t piece, const uint4& v) {
+    X* to_ = grad + r.at(piece);
+    if (vec) {
+      *reinterpret_cast<uint4*>(to_) = v;
+    } else {
+      X e[E];
+      __builtin_memcpy(e, &v, 16);
+#pragma unroll
+      for (int k = 0; k < E; ++k) to_[k] = e[k];
+    }
+  };
+  if (!counts) {
+    for (int32_t c = begin + tid; c < end; c += kPartThreads) put(c, make_uint4(0u, 0u, 0u, 0u));
+    if (loose >= 0) grad[loose] = X(0);
+    return;
+  }
+  for (int k = tid; k < ((a.K + 3) & ~3); k += kPartThreads) {
+    const int32_t id = k < a.K ? a.ids[t * a.K + k] : -1;
+    id_s[k] = id;
+    p_s[k] = k < a.K ? w.p[t * a.K + k] : 0.0f;
+  }
+  const float2 all =
+      join(lane < w.parts ? w.stats[t * w.parts + lane] : make_float2(-INFINITY, 0.0f), w.parts, k2);
+  const float M = __shfl(all.x, 0, 64), S = __shfl(all.y, 0, 64);
+  const float cw = a.weight / (float)a.len[sq] * a.inv_tau, f = cw * w.row[t].x / S;
+  auto scaled = [&](float x) { return f * exp2_hw((x - M) * k2); };
+  const float edge = loose >= 0 ? value(row[loose]) : 0.0f;
+  __syncthreads();
+  // the policy's logits that this part's entries name, before the gradient may
+  // take their place
+  auto in_part = [&](int32_t id) {
+    const int32_t p = (id - r.head) / E;
+    return id >= 0 && id < a.V &&
+           (id < r.head || p >= r.pieces ? part == 0 : p >= begin && p < end);
+  };
+  for (int k = tid; k < a.K; k += kPartThreads)
+    if (in_part(id_s[k])) z_s[k] = value(row[id_s[k]]);
+  __syncthreads();
+  for (int32_t c = begin + tid; c < end; c += kBatch * kPartThreads) {
+    uint4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * kPartThreads < end)
+        v[i] = *reinterpret_cast<const uint4*>(row + r.at(c + i * kPartThreads));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * kPartThreads < end) {
+        float x[E];
+        unpack(v[i], x);
+#pragma unroll
+        for (int k = 0; k < E; ++k) x[k] = scaled(x[k]);
+        put(c + i * kPartThreads, pack(x));
+      }
+  }
+  if (loose >= 0) to(grad[loose], scaled(edge));
+  __syncthreads();
+  for (int k = tid; k < a.K; k += kPartThreads)
+    if (in_part(id_s[k])) to(grad[id_s[k]], scaled(z_s[k]) - cw * mass_of(id_s[k], id_s, p_s, a.K));
 }
 
 // The sums over tokens, in one block and a fixed order.
@@ -389,13 +603,55 @@ void launch_rows(const X* z, X* dz, int64_t T, const Args& a, hipStream_t s) {
     go(integral_constant<int, 1024>{}, integral_constant<int, 20>{});
 }
 
+// Blocks that share a row, 1 for a block per row.  Sharing pays for up to 64 rows
+// of long vocabularies (bf16, one block against shared: 1 x 151936 23.4 / 10.0 us,
+// 32 24.6 / 15.3, 64 25.1 / 20.6, 128 28.4 / 32.0; 1 x 16000 11.0 / 9.5, 64 x 16000
+// fp32 10.6 / 11.6).  The type does not enter: a workspace is sized without it.
+int row_parts(int64_t T, int32_t V) {
+  int parts = 1;
+  if (T <= 64 && V >= 8192 && V >= 512 * T)
+    while (parts < 64 && T * parts < 512 && V / (2 * parts) >= 2048) parts *= 2;
+  return parts;
+}
+
+struct DistillWs {
+  float* terms;
+  PartsWs w;
+  size_t bytes;
+};
+
+DistillWs carve_distill(void* base, int64_t T, int32_t K, int32_t V) {
+  rbp::WsCarver c(base);
+  DistillWs d{};
+  d.w.parts = row_parts(T, V);
+  if (d.w.parts == 1) {
+    d.terms = c.take<float>((size_t)T * 2);
+  } else {
+    d.w.A = c.take<double>((size_t)T);
+    d.w.stats = c.take<float2>((size_t)T * d.w.parts);
+    d.w.row = c.take<float2>((size_t)T);
+    d.w.p = c.take<float>((size_t)T * K);
+  }
+  d.bytes = rbp::align_up(c.used, 256);
+  return d;
+}
+
+template <class X>
+void launch_parts(const X* z, X* dz, int64_t T, const Args& a, const PartsWs& w, float* loss_accum,
+                  float* stats, hipStream_t s) {
+  const int64_t blocks = T * w.parts;
+  hipLaunchKernelGGL(distill_part_kernel<X>, dim3((unsigned)blocks), dim3(kPartThreads), 0, s, z, a,
+                     w);
+  hipLaunchKernelGGL(distill_join_kernel<X>, dim3((unsigned)(dz == nullptr ? 1 : 1 + blocks)),
+                     dim3(kPartThreads), 0, s, z, dz, a, w, T, loss_accum, stats);
+}
+
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 }  // namespace
 
 size_t rbp::distill_ws(int64_t T, int32_t K, int32_t V) {
-  (void)K, (void)V;
-  return align_up((size_t)(T < 1 ? 1 : T) * 2 * sizeof(float), 256);
+  return carve_distill(nullptr, T < 1 ? 1 : T, K < 1 ? 1 : K, V < 1 ? 1 : V).bytes;
 }
 
 extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64_t ld,
@@ -427,15 +683,25 @@ extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64
   RBP_REQUIRE(ws && ws_bytes >= need, RBP_EWORKSPACE,
               "policy_distill_fwd_bwd: workspace needs %zu bytes, got %zu", need, ws_bytes);
   hipStream_t s = rbp::as_stream(stream);
-  float* terms = static_cast<float*>(ws);
+  const DistillWs d = carve_distill(ws, T, K, V);
   const Args a{ld, teacher_ids, teacher_logits, teacher_lse, seq_of_token, seq_len, V, K,
-               1.0f / temperature, (float)((double)scale / (double)n_seq_total), kl, terms};
+               1.0f / temperature, (float)((double)scale / (double)n_seq_total), kl, d.terms};
+  auto go = [&](auto type) {
+    using X = decltype(type);
+    const X* z = static_cast<const X*>(logits);
+    X* dz = static_cast<X*>(dlogits);
+    if (d.w.parts > 1) {
+      launch_parts(z, dz, T, a, d.w, loss_accum, stats, s);
+    } else {
+      launch_rows(z, dz, T, a, s);
+      hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, d.terms, kl, T, loss_accum,
+                         stats);
+    }
+  };
   if (logits_type == RBP_F32)
-    launch_rows(static_cast<const float*>(logits), static_cast<float*>(dlogits), T, a, s);
+    go(float{});
   else
-    launch_rows(static_cast<const uint16_t*>(logits), static_cast<uint16_t*>(dlogits), T, a, s);
-  hipLaunchKernelGGL(distill_sum_kernel, dim3(1), dim3(1024), 0, s, terms, kl, T, loss_accum,
-                     stats);
+    go(uint16_t{});
   RBP_CHECK_LAUNCH("policy_distill_fwd_bwd");
   return RBP_OK;
 }
