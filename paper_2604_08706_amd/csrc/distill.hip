@@ -10,15 +10,19 @@
 // one block reads it into registers, reduces it with a running reference and sum
 // as it arrives, and writes the gradient from there.
 
-#include "logits_epilogue.h"
 #include "rbp_internal.h"
+#include "vocab_rows.h"
 
 namespace {
 
-using rbp::lp::bf16_to_f32;
 using rbp::lp::exp2_hw;
 using rbp::lp::kLog2e;
-using rbp::lp::pack_bf16x2;
+using rbp::rows::aligned;
+using rbp::rows::pack;
+using rbp::rows::Row;
+using rbp::rows::to;
+using rbp::rows::unpack;
+using rbp::rows::value;
 
 constexpr int kMaxK = 256;
 
@@ -31,55 +35,6 @@ struct Args {
   float inv_tau, weight;  // weight = scale / n_seq
   float *kl, *terms;      // terms: [T][2] loss term, 1 if the token counts
 };
-
-// A row of logits as 16-byte pieces: the pieces that lie whole and aligned in
-// it, and up to 2 (E - 1) elements before and behind them.
-template <class X>
-struct Row {
-  static constexpr int E = 16 / sizeof(X);  // elements per piece
-  int32_t head, pieces, V;
-  __device__ __forceinline__ Row(const X* row, int32_t V_) : V(V_) {
-    const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(X));
-    head = (E - off) % E;
-    if (head > V) head = V;
-    pieces = (V - head) / E;
-  }
-  __device__ __forceinline__ int32_t at(int32_t piece) const { return head + piece * E; }
-  // the loose element that thread tid takes, -1 for none
-  __device__ __forceinline__ int32_t loose(int tid) const {
-    const int32_t v = tid < head ? tid : pieces * E + tid;
-    return tid < 2 * E && v < V ? v : -1;
-  }
-};
-
-__device__ __forceinline__ float value(float v) { return v; }
-__device__ __forceinline__ float value(uint16_t v) { return bf16_to_f32(v); }
-__device__ __forceinline__ void to(float& o, float v) { o = v; }
-__device__ __forceinline__ void to(uint16_t& o, float v) {
-  o = __builtin_bit_cast(uint16_t, (__bf16)v);
-}
-
-// A piece's elements, and back.
-__device__ __forceinline__ void unpack(const uint4& p, float (&x)[4]) {
-  x[0] = __uint_as_float(p.x), x[1] = __uint_as_float(p.y);
-  x[2] = __uint_as_float(p.z), x[3] = __uint_as_float(p.w);
-}
-__device__ __forceinline__ void unpack(const uint4& p, float (&x)[8]) {
-  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    x[2 * k] = __uint_as_float(w[k] << 16);
-    x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                    __float_as_uint(x[3]));
-}
-__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                    pack_bf16x2(x[6], x[7]));
-}
 
 // Running reference and sum of a thread: s = sum exp((z - m) inv_tau).  m follows
 // the largest logit only once that is kSlack (in powers of two) above it: sums
@@ -645,8 +600,6 @@ void launch_parts(const X* z, X* dz, int64_t T, const Args& a, const PartsWs& w,
   hipLaunchKernelGGL(distill_join_kernel<X>, dim3((unsigned)(dz == nullptr ? 1 : 1 + blocks)),
                      dim3(kPartThreads), 0, s, z, dz, a, w, T, loss_accum, stats);
 }
-
-inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 }  // namespace
 

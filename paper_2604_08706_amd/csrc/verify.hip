@@ -11,168 +11,567 @@
 // A running sum over 152064 tokens has steps of 1e-5 and less, and its rounding
 // decides which token a u beside a step draws: 32-bit sums would differ from the
 // exact ones in about one draw in a hundred.  So exponentials and sums are in 64
-// bits.
+// bits, whose multiply-adds this chip runs at the rate of 32-bit ones: 18
+// instructions per logit, about what the logit's load from HBM leaves time for.
+//
+// Up to three launches.  Every row is cut into segments of consecutive tokens, a
+// wave each (stats): the running sum of a whole row exists only by segments.
+// With a draft's logits, the weights max(p - q, 0) of the rejected position are
+// summed over the same segments (rest).  One block per sequence (finish) finds the
+// segment that u_K falls into, and the token inside it.
 
 #include <cmath>
 
-#include "logits_epilogue.h"
 #include "rbp_internal.h"
+#include "vocab_rows.h"
 
 namespace {
 
-using rbp::lp::bf16_to_f32;
+using rbp::rows::aligned;
+using rbp::rows::Row;
+using rbp::rows::unpack;
+using rbp::rows::value;
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
+constexpr double kLog2eD = 1.4426950408889634074;
+constexpr double kLn2 = 0.69314718055994530942;
 
-__device__ __forceinline__ double value(const float* p, int64_t i) { return (double)p[i]; }
-__device__ __forceinline__ double value(const uint16_t* p, int64_t i) {
-  return (double)bf16_to_f32(p[i]);
+// 2^y for y <= 1000: the nearest integer apart, a polynomial for the rest, whose
+// coefficients are a least-squares fit of the relative error on [-1/2, 1/2] that
+// was reweighted until it was level (1.5e-14), with 2^0 = 1 exactly.  -inf and
+// everything below -1100 give 0; so does a NaN (rows with one are found by their
+// largest logit).
+__device__ __forceinline__ double exp2_d(double y) {
+  y = fmax(y, -1100.0);
+  const double t = y + 0x1.8p52;
+  const double f = y - (t - 0x1.8p52);
+  double p = 0x1.b3dde4196d3a9p-24;
+  p = fma(p, f, 0x1.63e69a73f6558p-20);
+  p = fma(p, f, 0x1.ffce301d64a90p-17);
+  p = fma(p, f, 0x1.430897ef02c7ep-13);
+  p = fma(p, f, 0x1.5d87fd9362c75p-10);
+  p = fma(p, f, 0x1.3b2ab72414d27p-7);
+  p = fma(p, f, 0x1.c6b08d70c8985p-5);
+  p = fma(p, f, 0x1.ebfbdff81bde4p-3);
+  p = fma(p, f, 0x1.62e42fefa37d1p-1);
+  return __builtin_amdgcn_ldexp(fma(p, f, 1.0), __double2loint(t));
 }
 
-__device__ __forceinline__ double block_max(double v, double* s) {
-  for (int off = 32; off >= 1; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = s[0];
-  for (int w = 1; w < kWaves; ++w) v = fmax(v, s[w]);
-  return v;
-}
-__device__ __forceinline__ double block_sum(double v, double* s) {
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
   for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.0;
-  for (int w = 0; w < kWaves; ++w) v += s[w];
   return v;
 }
 
-// A row's distribution: exp((z - max) inv_tau) / sum; sum is NaN if the row has none.
-template <class X>
-struct Dist {
-  const X* z;
-  double inv_tau, max, sum;
-  __device__ void of(const X* row, int32_t V, double it, double* s) {
-    z = row;
-    inv_tau = it;
-    double m = -INFINITY;
-    for (int32_t v = threadIdx.x; v < V; v += kThreads) m = fmax(m, value(z, v));
-    max = block_max(m, s);
-    double e = 0.0;
-    for (int32_t v = threadIdx.x; v < V; v += kThreads) e += exp((value(z, v) - max) * inv_tau);
-    sum = block_sum(e, s);
-  }
-  __device__ double p(int64_t v) const { return exp((value(z, v) - max) * inv_tau) / sum; }
+// s = sum of 2^((z - m) k2) over some logits; m is -inf for none but -inf, and s
+// NaN where one is a NaN.
+struct Part {
+  double s;
+  float m, pad;
 };
 
-// One block per sequence.
+struct Args {
+  int64_t ld, ld_draft;
+  const int32_t *draft_tokens, *n_draft;
+  const float* u;
+  int32_t B, K, V, segments;
+  double k2;  // log2 e / temperature
+  int32_t* out_tokens;
+  float* out_logp;
+  int32_t* n_out;
+  Part* parts;   // [B][K + 1 + K][segments]: the policy's rows, then the draft's
+  double* rest;  // [B][segments]
+  __device__ __forceinline__ int32_t drafts(int64_t b) const {
+    return n_draft == nullptr ? K : min(n_draft[b], K);
+  }
+};
+
+// Tokens of a segment: whole pieces, with the loose elements at a row's ends.
 template <class X>
-__global__ void __launch_bounds__(kThreads) verify_kernel(
-    const X* __restrict__ logits, const X* __restrict__ draft_logits, int64_t ld, int64_t ld_draft,
-    const int32_t* __restrict__ draft_tokens, const int32_t* __restrict__ n_draft,
-    const float* __restrict__ u, int32_t K, int32_t V, double inv_tau,
-    int32_t* __restrict__ out_tokens, float* __restrict__ out_logp, int32_t* __restrict__ n_out) {
-  __shared__ double s[kWaves];
+struct Segment {
+  int32_t p0, p1, v0, v1;  // pieces, tokens
+  __device__ __forceinline__ Segment(const Row<X>& r, int seg, int n) {
+    p0 = (int32_t)((int64_t)r.pieces * seg / n);
+    p1 = (int32_t)((int64_t)r.pieces * (seg + 1) / n);
+    v0 = seg == 0 ? 0 : r.at(p0);
+    v1 = seg == n - 1 ? r.V : r.at(p1);
+  }
+};
+
+constexpr int kStatsThreads = 256;
+// the reference follows the largest logit once it is that many powers of two above
+constexpr float kSlack = 200.0f;
+
+// A wave per segment of a row.
+template <class X>
+__global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restrict__ logits,
+                                                              const X* __restrict__ draft_logits,
+                                                              Args a, int64_t n_items) {
+  constexpr int E = Row<X>::E, kBatch = 4;
+  const int64_t item = ((int64_t)blockIdx.x * kStatsThreads + threadIdx.x) >> 6;
+  if (item >= n_items) return;
+  const int lane = threadIdx.x & 63;
+  const int seg = (int)(item % a.segments);
+  const int rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
+  const int64_t row_id = item / a.segments;
+  const int64_t b = row_id / rows;
+  const int k = (int)(row_id % rows);
+  const int32_t n = a.drafts(b);
+  const bool drafted = k > a.K;
+  const int at = drafted ? k - a.K - 1 : k;
+  if (drafted ? at >= n : at > n) return;  // (n < 0: no row)
+  const X* row = drafted ? draft_logits + (b * a.K + at) * a.ld_draft
+                         : logits + (b * (a.K + 1) + at) * a.ld;
+  const Row<X> r(row, a.V);
+  const Segment<X> g(r, seg, a.segments);
+  const float slack = (float)fmin(kSlack / a.k2, 1e30);
+  float m = -INFINITY, top = -INFINITY;
+  double s = 0.0, ref = 0.0;  // m, or 0 while that is -inf
+  auto refer = [&](float largest) {
+    top = __builtin_elementwise_maximum(top, largest);
+    if (largest > m + slack) {
+      s *= exp2_d(((double)m - (double)largest) * a.k2);
+      m = largest;
+      ref = (double)m;
+    }
+  };
+  auto add = [&](const uint4& piece) {
+    float x[E];
+    unpack(piece, x);
+    float largest = x[0];
+#pragma unroll
+    for (int i = 1; i < E; ++i) largest = __builtin_elementwise_maximum(largest, x[i]);
+    refer(largest);
+    double e[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) e[i] = exp2_d(((double)x[i] - ref) * a.k2);
+#pragma unroll
+    for (int w = E / 2; w >= 1; w /= 2)
+#pragma unroll
+      for (int i = 0; i < w; ++i) e[i] += e[i + w];
+    s += e[0];
+  };
+  for (int32_t c = g.p0 + lane; c < g.p1; c += kBatch * 64) {
+    uint4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * 64 < g.p1) v[i] = *reinterpret_cast<const uint4*>(row + r.at(c + i * 64));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * 64 < g.p1) add(v[i]);
+  }
+  const int32_t loose = r.loose(lane);
+  if (loose >= 0 && (loose < r.head ? seg == 0 : seg == a.segments - 1)) {
+    const float x = value(row[loose]);
+    refer(x);
+    s += exp2_d(((double)x - ref) * a.k2);
+  }
+  float M = m;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    M = fmaxf(M, __shfl_xor(M, off, 64));
+    top = __builtin_elementwise_maximum(top, __shfl_xor(top, off, 64));
+  }
+  if (m != M) s *= exp2_d(((double)m - (double)M) * a.k2);
+  s = wave_sum(s);
+  if (lane == 0) a.parts[row_id * a.segments + seg] = Part{top != top ? (double)NAN : s, M, 0.0f};
+}
+
+// A row's reference and sum from its segments, by one wave; sum is NaN or 0 where
+// the row has no distribution.
+struct Dist {
+  double m, sum, ls;  // p = 2^((z - m) k2 - ls), ls = log2 sum
+  __device__ __forceinline__ double log2_of(float z, double k2) const {
+    return fma((double)z - m, k2, -ls);
+  }
+  __device__ __forceinline__ bool valid() const { return sum > 0.0 && sum < INFINITY; }
+};
+__device__ __forceinline__ Dist dist_of(const Part* parts, int n, double k2, int lane) {
+  const Part p = lane < n ? parts[lane] : Part{0.0, -INFINITY, 0.0f};
+  float M = p.m;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+  Dist d;
+  d.m = (double)M;
+  d.sum = wave_sum(p.m == M || p.s != p.s ? p.s : p.s * exp2_d(((double)p.m - (double)M) * k2));
+  if (!(M < INFINITY)) d.sum = NAN;
+  d.ls = log2(d.sum);
+  return d;
+}
+
+constexpr int kMaxK = 255;
+constexpr int kFinishThreads = 512;
+constexpr int kMaxSegments = 64;
+
+// What is decided of a sequence: drafts accepted, and the weights of the drawn
+// token: 0 p, 1 p without the draft, 2 max(p - q, 0); -1: no distribution.
+struct Decision {
+  int32_t accepted, kind, x;
+  Dist p, q;
+};
+
+// By a block, which takes the rows' distributions into LDS: the policy's of the
+// positions 0 .. n, then the draft's.
+template <class X>
+__device__ void decide(const X* __restrict__ logits, const X* __restrict__ draft_logits,
+                       const Args& a, int64_t b, int32_t n, Dist* rows_s, Decision* out) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
+  const Part* parts = a.parts + b * rows * a.segments;
+  for (int k = wave; k <= 2 * n; k += waves) {  // row k of the policy, or k - n - 1 of the draft
+    if (k > n && draft_logits == nullptr) break;
+    const int row = k <= n ? k : a.K + 1 + (k - n - 1);
+    const Dist d = dist_of(parts + row * a.segments, a.segments, a.k2, lane);
+    if (lane == 0) rows_s[k] = d;
+  }
+  __syncthreads();
+  // the first draft that is not accepted, 64 at a time
+  if (wave == 0) {
+    int32_t first = n;
+    for (int k0 = 0; k0 < n && first == n; k0 += 64) {
+      const int k = k0 + lane;
+      bool ok = true;
+      if (k < n) {
+        const int32_t x = a.draft_tokens[b * a.K + k];
+        const Dist p = rows_s[k];
+        ok = x >= 0 && x < a.V && p.valid();
+        if (ok) {
+          const double px =
+              exp2_d(p.log2_of(value(logits[(b * (a.K + 1) + k) * a.ld + x]), a.k2));
+          double qx = 1.0;
+          if (draft_logits != nullptr) {
+            const Dist q = rows_s[n + 1 + k];
+            qx = q.valid()
+                     ? exp2_d(q.log2_of(value(draft_logits[(b * a.K + k) * a.ld_draft + x]), a.k2))
+                     : NAN;
+          }
+          ok = (double)a.u[b * (a.K + 1) + k] * qx < px;
+        }
+      }
+      const uint64_t no = __ballot(!ok);
+      if (no != 0) first = k0 + __builtin_ctzll(no);
+    }
+    if (lane == 0) {
+      const bool drawn_from_p = first == n;
+      out->accepted = first;
+      out->x = drawn_from_p ? -1 : a.draft_tokens[b * a.K + first];
+      out->p = rows_s[first];
+      out->q = rows_s[drawn_from_p || draft_logits == nullptr ? first : n + 1 + first];
+      out->kind = !out->p.valid() ? -1
+                  : drawn_from_p ? 0
+                  : draft_logits == nullptr ? 1
+                  : out->q.valid() ? 2 : 0;
+    }
+  }
+  __syncthreads();
+}
+
+// The accepted drafts and their log-probs, -1 and 0 (NaN where there is nothing to
+// draw from) behind them, and the number of tokens.
+template <class X>
+__device__ __forceinline__ float logp_of(const X* row, int32_t x, const Dist& d, double k2) {
+  return (float)(kLn2 * d.log2_of(value(row[x]), k2));
+}
+template <class X>
+__device__ void emit_accepted(const X* __restrict__ logits, const Args& a, int64_t b,
+                              const Decision& d, const Dist* rows_s) {
+  for (int k = threadIdx.x; k <= a.K; k += blockDim.x) {
+    const int64_t i = b * (a.K + 1) + k;
+    const int32_t x = k < d.accepted ? a.draft_tokens[b * a.K + k] : -1;
+    a.out_tokens[i] = x;
+    a.out_logp[i] = x >= 0 ? logp_of(logits + i * a.ld, x, rows_s[k], a.k2)
+                    : k == d.accepted && d.kind < 0 ? NAN : 0.0f;
+  }
+  if (threadIdx.x == 0) a.n_out[b] = d.accepted + 1;
+}
+
+// Weight of token v under a decision.
+template <class X>
+struct Weight {
+  const X *p, *q;
+  double k2, mp, mq, lp, lq;
+  int32_t kind, x;
+  __device__ __forceinline__ double rest(float zp, float zq) const {
+    return fmax(exp2_d(fma((double)zp - mp, k2, -lp)) - exp2_d(fma((double)zq - mq, k2, -lq)), 0.0);
+  }
+  __device__ __forceinline__ double operator()(int32_t v) const {
+    const float z = value(p[v]);
+    if (kind == 2) return rest(z, value(q[v]));
+    return kind == 1 && v == x ? 0.0 : exp2_d(((double)z - mp) * k2);
+  }
+};
+template <class X>
+__device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logits,
+                                               const X* draft_logits, const Args& a, int64_t b) {
+  Weight<X> w;
+  w.p = logits + (b * (a.K + 1) + d.accepted) * a.ld;
+  w.q = d.kind == 2 ? draft_logits + (b * a.K + d.accepted) * a.ld_draft : nullptr;
+  w.k2 = a.k2;
+  // (p itself is drawn from unnormalised, as its segments' sums are)
+  w.mp = d.p.m;
+  w.lp = d.p.ls;
+  w.mq = d.q.m;
+  w.lq = d.q.ls;
+  w.kind = d.kind;
+  w.x = d.x;
+  return w;
+}
+
+constexpr int kRestThreads = 256;
+
+// Sums of max(p - q, 0) over the segments of the rejected position, a wave each.
+template <class X>
+__global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict__ logits,
+                                                            const X* __restrict__ draft_logits,
+                                                            Args a, Decision* decisions) {
+  __shared__ Dist rows_s[2 * kMaxK + 1];
+  __shared__ Decision d_s;
+  constexpr int kWaves = kRestThreads / 64;
+  const int blocks = (a.segments + kWaves - 1) / kWaves;
+  const int64_t b = blockIdx.x / blocks;
+  const int32_t n = a.drafts(b);
+  if (n < 0) return;
+  decide(logits, draft_logits, a, b, n, rows_s, &d_s);
+  const int part = blockIdx.x % blocks;
+  if (part == 0) {
+    if (threadIdx.x == 0) decisions[b] = d_s;
+    emit_accepted(logits, a, b, d_s, rows_s);
+  }
+  const int seg = part * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (d_s.kind != 2 || seg >= a.segments) return;
+  const Weight<X> w = weight_of(d_s, logits, draft_logits, a, b);
+  const Row<X> r(w.p, a.V);
+  const Segment<X> g(r, seg, a.segments);
+  // the pieces are the policy's row's; the draft's elements may lie otherwise
+  const bool vec =
+      ((reinterpret_cast<uintptr_t>(w.p) ^ reinterpret_cast<uintptr_t>(w.q)) & 15) == 0;
+  constexpr int E = Row<X>::E, kBatch = 2;
+  double s = 0.0;
+  for (int32_t c = g.p0 + lane; c < g.p1; c += kBatch * 64) {
+    uint4 zp[kBatch], zq[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (c + i * 64 >= g.p1) continue;
+      const int32_t at = r.at(c + i * 64);
+      zp[i] = *reinterpret_cast<const uint4*>(w.p + at);
+      if (vec) {
+        zq[i] = *reinterpret_cast<const uint4*>(w.q + at);
+      } else {
+        X e[E];
+#pragma unroll
+        for (int k = 0; k < E; ++k) e[k] = w.q[at + k];
+        __builtin_memcpy(&zq[i], e, 16);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (c + i * 64 >= g.p1) continue;
+      float p[E], q[E];
+      unpack(zp[i], p);
+      unpack(zq[i], q);
+#pragma unroll
+      for (int k = 0; k < E; ++k) s += w.rest(p[k], q[k]);
+    }
+  }
+  const int32_t loose = r.loose(lane);
+  if (loose >= 0 && (loose < r.head ? seg == 0 : seg == a.segments - 1)) s += w(loose);
+  s = wave_sum(s);
+  if (lane == 0) a.rest[b * a.segments + seg] = s;
+}
+
+// A block per sequence.
+template <class X>
+__global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restrict__ logits,
+                                                                const X* __restrict__ draft_logits,
+                                                                Args a,
+                                                                const Decision* decisions) {
+  constexpr int kWaves = kFinishThreads / 64;
+  __shared__ Dist rows_s[kMaxK + 1];
+  __shared__ Decision d_s;
+  __shared__ double seg_s[kMaxSegments], wave_s[kWaves];
   __shared__ int32_t found, last;
   const int64_t b = blockIdx.x;
-  const int tid = threadIdx.x;
-  int32_t n = n_draft == nullptr ? K : min(n_draft[b], K);
-  int32_t* tok = out_tokens + b * (K + 1);
-  float* lp = out_logp + b * (K + 1);
-  for (int k = tid; k <= K; k += kThreads) {
-    tok[k] = -1;
-    lp[k] = 0.0f;
-  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t n = a.drafts(b);
   if (n < 0) {
-    if (tid == 0) n_out[b] = 0;
+    for (int k = tid; k <= a.K; k += kFinishThreads) {
+      a.out_tokens[b * (a.K + 1) + k] = -1;
+      a.out_logp[b * (a.K + 1) + k] = 0.0f;
+    }
+    if (tid == 0) a.n_out[b] = 0;
     return;
+  }
+  const int rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
+  if (draft_logits == nullptr) {
+    decide(logits, draft_logits, a, b, n, rows_s, &d_s);
+    emit_accepted(logits, a, b, d_s, rows_s);
+  } else {
+    if (tid == 0) d_s = decisions[b];
+    __syncthreads();
+  }
+  if (d_s.kind < 0) return;
+  const int32_t accepted = d_s.accepted;
+  const X* row = logits + (b * (a.K + 1) + accepted) * a.ld;
+  const Row<X> r(row, a.V);
+  const Part* parts = a.parts + (b * rows + accepted) * a.segments;
+
+  // (each thread takes a run of a segment's tokens)
+  Weight<X> w = weight_of(d_s, logits, draft_logits, a, b);
+  auto run_of = [&](const Segment<X>& g, int32_t& v0, int32_t& v1) {
+    const int32_t each = (g.v1 - g.v0 + kFinishThreads - 1) / kFinishThreads;
+    v0 = min(g.v0 + tid * each, g.v1);
+    v1 = min(v0 + each, g.v1);
+  };
+  auto block_sum = [&](double v) {
+    v = wave_sum(v);
+    __syncthreads();
+    if (lane == 0) wave_s[wave] = v;
+    __syncthreads();
+    double sum = 0.0;
+    for (int q = 0; q < kWaves; ++q) sum += wave_s[q];
+    return sum;
+  };
+  auto p_segments = [&] {
+    if (tid < a.segments) {
+      const Part p = parts[tid];
+      seg_s[tid] = p.m == d_s.p.m ? p.s : p.s * exp2_d(((double)p.m - d_s.p.m) * a.k2);
+    }
+  };
+  if (w.kind == 2) {
+    if (tid < a.segments) seg_s[tid] = a.rest[b * a.segments + tid];
+  } else {
+    p_segments();
   }
   __syncthreads();
-  Dist<X> p, q;
-  int32_t a = 0, x = -1;
-  bool rejected = false;
-  for (;; ++a) {
-    p.of(logits + (b * (K + 1) + a) * ld, V, inv_tau, s);
-    if (a == n) break;
-    x = draft_tokens[b * K + a];
-    const bool in = x >= 0 && x < V;
-    if (draft_logits != nullptr) q.of(draft_logits + (b * K + a) * ld_draft, V, inv_tau, s);
-    const double px = in ? p.p(x) : 0.0;
-    const double qx = draft_logits == nullptr ? 1.0 : in ? q.p(x) : 0.0;
-    if (!((double)u[b * (K + 1) + a] * qx < px)) {
-      rejected = true;
-      break;
-    }
-    if (tid == 0) {
-      tok[a] = x;
-      lp[a] = (float)log(px);
-    }
+  if (w.kind == 1) {  // the draft's segment without the draft
+    int seg = 0;
+    for (; seg < a.segments - 1; ++seg)
+      if (w.x < Segment<X>(r, seg, a.segments).v1) break;
+    int32_t v0, v1;
+    run_of(Segment<X>(r, seg, a.segments), v0, v1);
+    double s = 0.0;
+    for (int32_t v = v0; v < v1; ++v) s += w(v);
+    s = block_sum(s);
+    __syncthreads();
+    if (tid == 0) seg_s[seg] = s;
+    __syncthreads();
   }
-  if (tid == 0) n_out[b] = a + 1;
-  if (!(p.sum > 0.0 && p.sum < INFINITY)) {
-    if (tid == 0) lp[a] = NAN;
-    return;
-  }
-  int kind = !rejected ? 0 : draft_logits == nullptr ? 1 : q.sum > 0.0 ? 2 : 0;
-  auto weight = [&](int32_t v) {
-    const double pv = p.p(v);
-    return kind == 0 ? pv : kind == 1 ? (v == x ? 0.0 : pv) : fmax(pv - q.p(v), 0.0);
+  // running sums over the segments, a lane each
+  double mine, scan;
+  auto scan_segments = [&] {
+    mine = lane < a.segments ? seg_s[lane] : 0.0;
+    scan = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const double o = __shfl_up(scan, off, 64);
+      if (lane >= off) scan += o;
+    }
+    return __shfl(scan, 63, 64);
   };
-  double total = 0.0;
-  for (;;) {
-    double e = 0.0;
-    for (int32_t v = tid; v < V; v += kThreads) e += weight(v);
-    total = block_sum(e, s);
-    if (total > 0.0 || kind == 0) break;
-    kind = 0;
+  double total = scan_segments();
+  if (w.kind != 0 && !(total > 0.0)) {  // nothing left: draw from p
+    __syncthreads();
+    d_s.kind = 0;
+    w = weight_of(d_s, logits, draft_logits, a, b);
+    p_segments();
+    __syncthreads();
+    total = scan_segments();
   }
-  const double goal = (double)u[b * (K + 1) + K] * total;
+  const double goal = (double)a.u[b * (a.K + 1) + a.K] * total;
   if (tid == 0) {
-    found = V;
+    found = a.V;
     last = -1;
   }
-  __syncthreads();
-  double before = 0.0;
-  for (int32_t v0 = 0; v0 < V; v0 += kThreads) {
-    const int32_t v = v0 + tid;
-    const double wv = v < V ? weight(v) : 0.0;
-    double run = wv;  // inclusive over the tile
+  // The first segment whose end lies behind the goal; after it the next ones, should
+  // rounding leave the token to them; the last with any weight where none does (u at
+  // the end of its interval).
+  const uint64_t some = __ballot(mine > 0.0), behind = __ballot(mine > 0.0 && scan > goal);
+  for (uint64_t todo = behind != 0 ? behind : 1ull << (63 - __builtin_clzll(some)); todo != 0;
+       todo &= todo - 1) {
+    const int seg = __builtin_ctzll(todo);
+    int32_t v0, v1;
+    run_of(Segment<X>(r, seg, a.segments), v0, v1);
+    double s = 0.0;
+    for (int32_t v = v0; v < v1; ++v) s += w(v);
+    double upto = s;  // inclusive over the wave
+#pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-      const double o = __shfl_up(run, off, 64);
-      if ((tid & 63) >= off) run += o;
+      const double o = __shfl_up(upto, off, 64);
+      if (lane >= off) upto += o;
     }
     __syncthreads();
-    if ((tid & 63) == 63) s[tid >> 6] = run;
+    if (lane == 63) wave_s[wave] = upto;
     __syncthreads();
-    double tile = 0.0;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < (tid >> 6)) run += s[w];
-      tile += s[w];
+    double run = seg > 0 ? __shfl(scan, seg - 1, 64) : 0.0;
+    for (int q = 0; q < wave; ++q) run += wave_s[q];
+    run += upto - s;
+    int32_t hit = a.V, end = -1;
+    for (int32_t v = v0; v < v1; ++v) {
+      const double wv = w(v);
+      run += wv;
+      if (wv > 0.0) {
+        end = v;
+        if (run > goal) {
+          hit = v;
+          break;
+        }
+      }
     }
-    if (wv > 0.0) {
-      atomicMax(&last, v);
-      if (before + run > goal) atomicMin(&found, v);
-    }
-    before += tile;
+    if (hit < a.V) atomicMin(&found, hit);
+    if (end >= 0) atomicMax(&last, end);
     __syncthreads();
-    if (found < V) break;
+    if (found < a.V) break;
   }
   if (tid == 0) {
-    const int32_t v = found < V ? found : last;
-    tok[a] = v;
-    lp[a] = v < 0 ? NAN : (float)log(p.p(v));
+    const int64_t i = b * (a.K + 1) + accepted;
+    const int32_t v = found < a.V ? found : last;
+    a.out_tokens[i] = v;
+    a.out_logp[i] = logp_of(row, v, d_s.p, a.k2);
   }
 }
 
-inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+// Segments of a row: 512 tokens or more each, a wave's lanes to join them.
+int segments_of(int32_t V) {
+  int n = 1;
+  while (n < kMaxSegments && V / (2 * n) >= 512) n *= 2;
+  return n;
+}
+
+struct VerifyWs {
+  Part* parts;
+  double* rest;
+  Decision* decisions;
+  size_t bytes;
+};
+VerifyWs carve_verify(void* base, int64_t B, int64_t K, int32_t V) {
+  rbp::WsCarver c(base);
+  VerifyWs w;
+  const size_t segments = (size_t)segments_of(V);
+  w.parts = c.take<Part>((size_t)B * (2 * K + 1) * segments);
+  w.rest = c.take<double>((size_t)B * segments);
+  w.decisions = c.take<Decision>((size_t)B);
+  w.bytes = rbp::align_up(c.used, 256);
+  return w;
+}
+
+template <class X>
+void launch(const X* logits, const X* draft_logits, const Args& a, Decision* decisions,
+            hipStream_t s) {
+  const int64_t rows = a.B * (int64_t)(draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1);
+  const int64_t items = rows * a.segments;
+  hipLaunchKernelGGL(stats_kernel<X>, dim3((unsigned)rbp::ceil_div(items, kStatsThreads / 64)),
+                     dim3(kStatsThreads), 0, s, logits, draft_logits, a, items);
+  if (draft_logits != nullptr)
+    hipLaunchKernelGGL(rest_kernel<X>,
+                       dim3((unsigned)(a.B * rbp::ceil_div(a.segments, kRestThreads / 64))),
+                       dim3(kRestThreads), 0, s, logits, draft_logits, a, decisions);
+  hipLaunchKernelGGL(finish_kernel<X>, dim3(a.B), dim3(kFinishThreads), 0, s, logits, draft_logits,
+                     a, decisions);
+}
 
 }  // namespace
 
 size_t rbp::verify_ws(int64_t B, int32_t K, int32_t V) {
-  (void)B, (void)K, (void)V;
-  return 256;
+  return carve_verify(nullptr, B < 1 ? 1 : B, K < 0 ? 0 : K, V < 1 ? 1 : V).bytes;
 }
 
 extern "C" int policy_verify_drafts(const void* logits, const void* draft_logits, int logits_type,
@@ -200,17 +599,17 @@ extern "C" int policy_verify_drafts(const void* logits, const void* draft_logits
   RBP_REQUIRE(ws && ws_bytes >= need, RBP_EWORKSPACE,
               "policy_verify_drafts: workspace needs %zu bytes, got %zu", need, ws_bytes);
   hipStream_t s = rbp::as_stream(stream);
-  const double inv_tau = 1.0 / (double)temperature;
+  const VerifyWs w = carve_verify(ws, B, K, V);
+  if (K == 0) draft_logits = nullptr;
+  const Args a{ld,       ld_draft, draft_tokens, n_draft, u,       B,          K,
+               V,        segments_of(V), kLog2eD / (double)temperature, out_tokens, out_logp,
+               n_out,    w.parts,  w.rest};
   if (logits_type == RBP_F32)
-    hipLaunchKernelGGL(verify_kernel<float>, dim3(B), dim3(kThreads), 0, s,
-                       static_cast<const float*>(logits), static_cast<const float*>(draft_logits),
-                       ld, ld_draft, draft_tokens, n_draft, u, K, V, inv_tau, out_tokens, out_logp,
-                       n_out);
+    launch(static_cast<const float*>(logits), static_cast<const float*>(draft_logits), a,
+           w.decisions, s);
   else
-    hipLaunchKernelGGL(verify_kernel<uint16_t>, dim3(B), dim3(kThreads), 0, s,
-                       static_cast<const uint16_t*>(logits),
-                       static_cast<const uint16_t*>(draft_logits), ld, ld_draft, draft_tokens,
-                       n_draft, u, K, V, inv_tau, out_tokens, out_logp, n_out);
+    launch(static_cast<const uint16_t*>(logits), static_cast<const uint16_t*>(draft_logits), a,
+           w.decisions, s);
   RBP_CHECK_LAUNCH("policy_verify_drafts");
   return RBP_OK;
 }
