@@ -11,8 +11,9 @@
 // A running sum over 152064 tokens has steps of 1e-5 and less, and its rounding
 // decides which token a u beside a step draws: 32-bit sums would differ from the
 // exact ones in about one draw in a hundred.  So exponentials and sums are in 64
-// bits, whose multiply-adds this chip runs at the rate of 32-bit ones: 18
-// instructions per logit, about what the logit's load from HBM leaves time for.
+// bits, whose operations this chip runs at the rate of 32-bit ones (52 lanes a clock
+// and compute unit measured): about 17 per logit, near what its load from HBM
+// leaves time for.
 //
 // Up to three launches.  Every row is cut into segments of consecutive tokens, a
 // wave each (stats): the running sum of a whole row exists only by segments.
@@ -35,11 +36,11 @@ using rbp::rows::value;
 constexpr double kLog2eD = 1.4426950408889634074;
 constexpr double kLn2 = 0.69314718055994530942;
 
-// 2^y for y <= 1000: the nearest integer apart, a polynomial for the rest, whose
-// coefficients are a least-squares fit of the relative error on [-1/2, 1/2] that
-// was reweighted until it was level (1.5e-14), with 2^0 = 1 exactly.  -inf and
-// everything below -1100 give 0; so does a NaN (rows with one are found by their
-// largest logit).
+// 2^y for y <= 1000, to 1.5e-14: the nearest integer apart, a polynomial for the
+// rest, whose coefficients are a least-squares fit of the relative error on
+// [-1/2, 1/2] that was reweighted until it was level, with 2^0 = 1 exactly.  -inf
+// and everything below -1100 give 0; so does a NaN (rows with one are found by
+// their largest logit).
 __device__ __forceinline__ double exp2_d(double y) {
   y = fmax(y, -1100.0);
   const double t = y + 0x1.8p52;
@@ -56,14 +57,85 @@ __device__ __forceinline__ double exp2_d(double y) {
   return __builtin_amdgcn_ldexp(fma(p, f, 1.0), __double2loint(t));
 }
 
+// The same where whole rows are summed, to 8e-14: 2^(x k2) as a power of two, a root
+// from a table of 32 in LDS (banks of their own: no conflicts; 128 roots and one
+// multiplication less took as long), and a polynomial of degree 4 instead of 9, fitted
+// likewise.  With n = rint(32 x k2), the sum of 32 x k2 and 1.5 2^52 - c (c an integer
+// near the reference's 32 ref k2) holds n - c in its low bits: three operations for n
+// and the fraction, exact before the last rounding.
+constexpr int kRoots = 32;
+__constant__ double g_roots[kRoots] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+struct Scaled {
+  double p, root;  // their product is 2^(x k2 - c / 32)
+};
+struct Grid {
+  double k, c;   // 32 k2; 1.5 2^52 minus the integer
+  double shift;  // (the integer) / 32
+  float floor;   // logits below are taken for this one: 2^-1000 beside the reference
+  // Whether the reference and the temperature allow it; where not (logits beyond
+  // 2^24 temperatures, temperatures beyond 1e27) exp2_d serves.
+  bool near;
+  __device__ __forceinline__ void refer(double ref, double k2, double span) {
+    k = kRoots * k2;
+    const double n = rint(ref * k);
+    c = 0x1.8p52 - n;
+    shift = n * (1.0 / kRoots);
+    const double low = ref - span;
+    near = fabs(ref) * k2 < 0x1p24 && low > -1e30;
+    floor = (float)low;
+  }
+  // Exponentials of N logits: the roots' loads of all, then the polynomials.
+  template <int N>
+  __device__ __forceinline__ void operator()(const float (&z)[N], const double* roots,
+                                             Scaled (&y)[N]) const {
+    double f[N], r[N];
+    int n[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      // (fmaxf would quiet each operand first; a NaN may pass)
+      float x;
+      asm("v_max_f32 %0, %1, %2" : "=v"(x) : "v"(z[i]), "v"(floor));
+      const double t = fma((double)x, k, c);
+      f[i] = fma((double)x, k, c - t);
+      n[i] = __double2loint(t);
+      r[i] = roots[n[i] & (kRoots - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      double p = 0x1.3b2aa27434ff1p-27;
+      p = fma(p, f[i], 0x1.c6b167e2738bcp-20);
+      p = fma(p, f[i], 0x1.ebfbdff87858dp-13);
+      p = fma(p, f[i], 0x1.62e42fef6d042p-6);
+      y[i].p = fma(p, f[i], 1.0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      // the power of two goes into the exponent, which stays in range
+      int hi;
+      asm("v_lshl_add_u32 %0, %1, 15, %2"
+          : "=v"(hi)
+          : "v"(n[i] & ~(kRoots - 1)), "v"(__double2hiint(r[i])));
+      y[i].root = __hiloint2double(hi, __double2loint(r[i]));
+    }
+  }
+};
+
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
   return v;
 }
 
-// s = sum of 2^((z - m) k2) over some logits; m is -inf for none but -inf, and s
-// NaN where one is a NaN.
+// s = sum of 2^((z - m) k2) over some logits; m = -inf and s = 0 for none but
+// -inf, and s a NaN where one is.
 struct Part {
   double s;
   float m, pad;
@@ -73,13 +145,15 @@ struct Args {
   int64_t ld, ld_draft;
   const int32_t *draft_tokens, *n_draft;
   const float* u;
-  int32_t B, K, V, segments;
-  double k2;  // log2 e / temperature
+  int32_t B, K, V, segments, log_segments;
+  double k2;    // log2 e / temperature
+  double span;  // 1000 / k2
+  float slack;  // kSlack / k2
   int32_t* out_tokens;
   float* out_logp;
   int32_t* n_out;
   Part* parts;   // [B][K + 1 + K][segments]: the policy's rows, then the draft's
-  double* rest;  // [B][segments]
+  double* rest;  // [B][segments][kShares]
   __device__ __forceinline__ int32_t drafts(int64_t b) const {
     return n_draft == nullptr ? K : min(n_draft[b], K);
   }
@@ -89,17 +163,17 @@ struct Args {
 template <class X>
 struct Segment {
   int32_t p0, p1, v0, v1;  // pieces, tokens
-  __device__ __forceinline__ Segment(const Row<X>& r, int seg, int n) {
-    p0 = (int32_t)((int64_t)r.pieces * seg / n);
-    p1 = (int32_t)((int64_t)r.pieces * (seg + 1) / n);
+  __device__ __forceinline__ Segment(const Row<X>& r, int seg, int log_n) {
+    p0 = (int32_t)(((int64_t)r.pieces * seg) >> log_n);
+    p1 = (int32_t)(((int64_t)r.pieces * (seg + 1)) >> log_n);
     v0 = seg == 0 ? 0 : r.at(p0);
-    v1 = seg == n - 1 ? r.V : r.at(p1);
+    v1 = (seg + 1) >> log_n ? r.V : r.at(p1);
   }
 };
 
 constexpr int kStatsThreads = 256;
 // the reference follows the largest logit once it is that many powers of two above
-constexpr float kSlack = 200.0f;
+constexpr double kSlack = 200.0;
 
 // A wave per segment of a row.
 template <class X>
@@ -107,12 +181,17 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
                                                               const X* __restrict__ draft_logits,
                                                               Args a, int64_t n_items) {
   constexpr int E = Row<X>::E, kBatch = 4;
-  const int64_t item = ((int64_t)blockIdx.x * kStatsThreads + threadIdx.x) >> 6;
+  // (rows times segments may pass 31 bits, rows may not)
+  const int64_t item = (int64_t)blockIdx.x * (kStatsThreads / 64) +
+                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ double roots[kRoots];
+  if (threadIdx.x < kRoots) roots[threadIdx.x] = g_roots[threadIdx.x];
+  __syncthreads();
   if (item >= n_items) return;
   const int lane = threadIdx.x & 63;
-  const int seg = (int)(item % a.segments);
-  const int rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
-  const int64_t row_id = item / a.segments;
+  const int seg = (int)(item & (a.segments - 1));
+  const uint32_t rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
+  const uint32_t row_id = (uint32_t)(item >> a.log_segments);
   const int64_t b = row_id / rows;
   const int k = (int)(row_id % rows);
   const int32_t n = a.drafts(b);
@@ -122,16 +201,23 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
   const X* row = drafted ? draft_logits + (b * a.K + at) * a.ld_draft
                          : logits + (b * (a.K + 1) + at) * a.ld;
   const Row<X> r(row, a.V);
-  const Segment<X> g(r, seg, a.segments);
-  const float slack = (float)fmin(kSlack / a.k2, 1e30);
+  const Segment<X> g(r, seg, a.log_segments);
   float m = -INFINITY, top = -INFINITY;
-  double s = 0.0, ref = 0.0;  // m, or 0 while that is -inf
+  double s = 0.0;  // relative to 2^(grid.shift), or to the reference where that is far
+  Grid grid;
+  grid.refer(0.0, a.k2, a.span);
   auto refer = [&](float largest) {
     top = __builtin_elementwise_maximum(top, largest);
-    if (largest > m + slack) {
-      s *= exp2_d(((double)m - (double)largest) * a.k2);
+    if (largest > m + a.slack) {
+      const Grid old = grid;
+      grid.refer((double)largest, a.k2, a.span);
+      if (m == -INFINITY)
+        s = 0.0;
+      else if (old.near && grid.near)
+        s *= exp2_d(old.shift - grid.shift);
+      else
+        s *= exp2_d((old.near ? old.shift : (double)m * a.k2) - (double)largest * a.k2);
       m = largest;
-      ref = (double)m;
     }
   };
   auto add = [&](const uint4& piece) {
@@ -141,14 +227,21 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
 #pragma unroll
     for (int i = 1; i < E; ++i) largest = __builtin_elementwise_maximum(largest, x[i]);
     refer(largest);
-    double e[E];
+    if (!grid.near) {
+#pragma unroll 1
+      for (int i = 0; i < E; ++i) {
+        s += exp2_d(((double)x[0] - (double)m) * a.k2);
 #pragma unroll
-    for (int i = 0; i < E; ++i) e[i] = exp2_d(((double)x[i] - ref) * a.k2);
+        for (int j = 1; j < E; ++j) x[j - 1] = x[j];
+      }
+      return;
+    }
+    double e[4] = {s, 0.0, 0.0, 0.0};  // sums of their own: no chain of 8 additions
+    Scaled y[E];
+    grid(x, roots, y);
 #pragma unroll
-    for (int w = E / 2; w >= 1; w /= 2)
-#pragma unroll
-      for (int i = 0; i < w; ++i) e[i] += e[i + w];
-    s += e[0];
+    for (int i = 0; i < E; ++i) e[i & 3] = fma(y[i].p, y[i].root, e[i & 3]);
+    s = (e[0] + e[1]) + (e[2] + e[3]);
   };
   for (int32_t c = g.p0 + lane; c < g.p1; c += kBatch * 64) {
     uint4 v[kBatch];
@@ -163,7 +256,7 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
   if (loose >= 0 && (loose < r.head ? seg == 0 : seg == a.segments - 1)) {
     const float x = value(row[loose]);
     refer(x);
-    s += exp2_d(((double)x - ref) * a.k2);
+    s += exp2_d(grid.near ? fma((double)x, a.k2, -grid.shift) : ((double)x - (double)m) * a.k2);
   }
   float M = m;
 #pragma unroll
@@ -171,9 +264,13 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
     M = fmaxf(M, __shfl_xor(M, off, 64));
     top = __builtin_elementwise_maximum(top, __shfl_xor(top, off, 64));
   }
-  if (m != M) s *= exp2_d(((double)m - (double)M) * a.k2);
+  // relative to the largest reference
+  s = m == -INFINITY ? 0.0
+      : s * exp2_d(grid.near ? fma((double)-M, a.k2, grid.shift)
+                             : ((double)m - (double)M) * a.k2);
   s = wave_sum(s);
-  if (lane == 0) a.parts[row_id * a.segments + seg] = Part{top != top ? (double)NAN : s, M, 0.0f};
+  if (lane == 0)
+    a.parts[(int64_t)row_id * a.segments + seg] = Part{top != top ? (double)NAN : s, M, 0.0f};
 }
 
 // A row's reference and sum from its segments, by one wave; sum is NaN or 0 where
@@ -199,7 +296,9 @@ __device__ __forceinline__ Dist dist_of(const Part* parts, int n, double k2, int
 }
 
 constexpr int kMaxK = 255;
-constexpr int kFinishThreads = 512;
+constexpr int kShares = 2;  // waves of a segment in rest_kernel
+constexpr int kFinishThreads = 1024;
+constexpr int kRun = 5;  // tokens of a thread: a segment of 152064 / 32 in one tile
 constexpr int kMaxSegments = 64;
 
 // What is decided of a sequence: drafts accepted, and the weights of the drawn
@@ -293,11 +392,6 @@ struct Weight {
   __device__ __forceinline__ double rest(float zp, float zq) const {
     return fmax(exp2_d(fma((double)zp - mp, k2, -lp)) - exp2_d(fma((double)zq - mq, k2, -lq)), 0.0);
   }
-  __device__ __forceinline__ double operator()(int32_t v) const {
-    const float z = value(p[v]);
-    if (kind == 2) return rest(z, value(q[v]));
-    return kind == 1 && v == x ? 0.0 : exp2_d(((double)z - mp) * k2);
-  }
 };
 template <class X>
 __device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logits,
@@ -308,15 +402,15 @@ __device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logit
   w.k2 = a.k2;
   // (p itself is drawn from unnormalised, as its segments' sums are)
   w.mp = d.p.m;
-  w.lp = d.p.ls;
-  w.mq = d.q.m;
-  w.lq = d.q.ls;
+  w.lp = d.kind == 2 ? d.p.ls : 0.0;
+  w.mq = d.kind == 2 ? d.q.m : 0.0;
+  w.lq = d.kind == 2 ? d.q.ls : 0.0;
   w.kind = d.kind;
   w.x = d.x;
   return w;
 }
 
-constexpr int kRestThreads = 256;
+constexpr int kRestThreads = 512;
 
 // Sums of max(p - q, 0) over the segments of the rejected position, a wave each.
 template <class X>
@@ -325,8 +419,10 @@ __global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict_
                                                             Args a, Decision* decisions) {
   __shared__ Dist rows_s[2 * kMaxK + 1];
   __shared__ Decision d_s;
+  __shared__ double roots[kRoots];
   constexpr int kWaves = kRestThreads / 64;
-  const int blocks = (a.segments + kWaves - 1) / kWaves;
+  if (threadIdx.x < kRoots) roots[threadIdx.x] = g_roots[threadIdx.x];
+  const unsigned blocks = (a.segments * kShares + kWaves - 1) / kWaves;
   const int64_t b = blockIdx.x / blocks;
   const int32_t n = a.drafts(b);
   if (n < 0) return;
@@ -336,21 +432,31 @@ __global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict_
     if (threadIdx.x == 0) decisions[b] = d_s;
     emit_accepted(logits, a, b, d_s, rows_s);
   }
-  const int seg = part * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int item = part * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int seg = item / kShares, share = item % kShares;
   if (d_s.kind != 2 || seg >= a.segments) return;
   const Weight<X> w = weight_of(d_s, logits, draft_logits, a, b);
   const Row<X> r(w.p, a.V);
-  const Segment<X> g(r, seg, a.segments);
+  const Segment<X> g(r, seg, a.log_segments);
   // the pieces are the policy's row's; the draft's elements may lie otherwise
   const bool vec =
       ((reinterpret_cast<uintptr_t>(w.p) ^ reinterpret_cast<uintptr_t>(w.q)) & 15) == 0;
   constexpr int E = Row<X>::E, kBatch = 2;
+  // p = 2^(z k2 - shift) cp, and q likewise: max(p - q, 0) = cp max(.. - .. cq / cp, 0)
+  Grid gp, gq;
+  gp.refer(w.mp, a.k2, a.span);
+  gq.refer(w.mq, a.k2, a.span);
+  const bool near = gp.near && gq.near;
+  const double cp = near ? exp2_d(fma(-w.mp, a.k2, gp.shift) - w.lp) : 1.0;
+  const double ratio = near ? exp2_d(fma(-w.mq, a.k2, gq.shift) - w.lq) / cp : 1.0;
   double s = 0.0;
-  for (int32_t c = g.p0 + lane; c < g.p1; c += kBatch * 64) {
+  const int32_t p0 = g.p0 + (g.p1 - g.p0) * share / kShares,
+                p1 = g.p0 + (g.p1 - g.p0) * (share + 1) / kShares;
+  for (int32_t c = p0 + lane; c < p1; c += kBatch * 64) {
     uint4 zp[kBatch], zq[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      if (c + i * 64 >= g.p1) continue;
+      if (c + i * 64 >= p1) continue;
       const int32_t at = r.at(c + i * 64);
       zp[i] = *reinterpret_cast<const uint4*>(w.p + at);
       if (vec) {
@@ -362,20 +468,37 @@ __global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict_
         __builtin_memcpy(&zq[i], e, 16);
       }
     }
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < kBatch; ++i) {
-      if (c + i * 64 >= g.p1) continue;
-      float p[E], q[E];
-      unpack(zp[i], p);
-      unpack(zq[i], q);
+      if (c + i * 64 < p1) {
+        float p[E], q[E];
+        unpack(zp[0], p);
+        unpack(zq[0], q);
+        if (near) {
+          Scaled e[E], f[E];
+          gp(p, roots, e);
+          gq(q, roots, f);
 #pragma unroll
-      for (int k = 0; k < E; ++k) s += w.rest(p[k], q[k]);
+          for (int k = 0; k < E; ++k)
+            s += fmax(fma(e[k].p, e[k].root, -(f[k].p * ratio) * f[k].root), 0.0);
+        } else {
+#pragma unroll 1
+          for (int k = 0; k < E; ++k) {
+            s += w.rest(p[0], q[0]);
+#pragma unroll
+            for (int j = 1; j < E; ++j) p[j - 1] = p[j], q[j - 1] = q[j];
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 1; k < kBatch; ++k) zp[k - 1] = zp[k], zq[k - 1] = zq[k];
     }
   }
   const int32_t loose = r.loose(lane);
-  if (loose >= 0 && (loose < r.head ? seg == 0 : seg == a.segments - 1)) s += w(loose);
-  s = wave_sum(s);
-  if (lane == 0) a.rest[b * a.segments + seg] = s;
+  if (share == 0 && loose >= 0 && (loose < r.head ? seg == 0 : seg == a.segments - 1))
+    s += w.rest(value(w.p[loose]), value(w.q[loose])) / cp;
+  s = wave_sum(s) * cp;
+  if (lane == 0) a.rest[b * a.segments * kShares + item] = s;
 }
 
 // A block per sequence.
@@ -387,11 +510,19 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
   constexpr int kWaves = kFinishThreads / 64;
   __shared__ Dist rows_s[kMaxK + 1];
   __shared__ Decision d_s;
-  __shared__ double seg_s[kMaxSegments], wave_s[kWaves];
+  __shared__ double seg_s[kMaxSegments], wave_s[kWaves], wt_s[kRun][kFinishThreads];
   __shared__ int32_t found, last;
   const int64_t b = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t n = a.drafts(b);
+  const double u = (double)a.u[b * (a.K + 1) + a.K];
+  // (what the rest's launch left, should there be one: loaded with the decision)
+  double rest = 0.0;
+  if (draft_logits != nullptr && tid < a.segments) {
+    static_assert(kShares == 2, "two sums");
+    const double* q = a.rest + (b * a.segments + tid) * kShares;
+    rest = q[0] + q[1];
+  }
   if (n < 0) {
     for (int k = tid; k <= a.K; k += kFinishThreads) {
       a.out_tokens[b * (a.K + 1) + k] = -1;
@@ -414,125 +545,162 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
   const Row<X> r(row, a.V);
   const Part* parts = a.parts + (b * rows + accepted) * a.segments;
 
-  // (each thread takes a run of a segment's tokens)
   Weight<X> w = weight_of(d_s, logits, draft_logits, a, b);
-  auto run_of = [&](const Segment<X>& g, int32_t& v0, int32_t& v1) {
-    const int32_t each = (g.v1 - g.v0 + kFinishThreads - 1) / kFinishThreads;
-    v0 = min(g.v0 + tid * each, g.v1);
-    v1 = min(v0 + each, g.v1);
-  };
-  auto block_sum = [&](double v) {
-    v = wave_sum(v);
-    __syncthreads();
-    if (lane == 0) wave_s[wave] = v;
-    __syncthreads();
-    double sum = 0.0;
-    for (int q = 0; q < kWaves; ++q) sum += wave_s[q];
-    return sum;
-  };
-  auto p_segments = [&] {
+  auto segments_of_p = [&] {
     if (tid < a.segments) {
       const Part p = parts[tid];
       seg_s[tid] = p.m == d_s.p.m ? p.s : p.s * exp2_d(((double)p.m - d_s.p.m) * a.k2);
     }
   };
   if (w.kind == 2) {
-    if (tid < a.segments) seg_s[tid] = a.rest[b * a.segments + tid];
+    // (2^-1000 a token, where they have nothing left)
+    if (tid < a.segments) seg_s[tid] = rest > 0x1p-900 ? rest : 0.0;
   } else {
-    p_segments();
+    segments_of_p();
   }
-  __syncthreads();
-  if (w.kind == 1) {  // the draft's segment without the draft
-    int seg = 0;
-    for (; seg < a.segments - 1; ++seg)
-      if (w.x < Segment<X>(r, seg, a.segments).v1) break;
-    int32_t v0, v1;
-    run_of(Segment<X>(r, seg, a.segments), v0, v1);
-    double s = 0.0;
-    for (int32_t v = v0; v < v1; ++v) s += w(v);
-    s = block_sum(s);
-    __syncthreads();
-    if (tid == 0) seg_s[seg] = s;
-    __syncthreads();
-  }
-  // running sums over the segments, a lane each
-  double mine, scan;
-  auto scan_segments = [&] {
-    mine = lane < a.segments ? seg_s[lane] : 0.0;
-    scan = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const double o = __shfl_up(scan, off, 64);
-      if (lane >= off) scan += o;
-    }
-    return __shfl(scan, 63, 64);
-  };
-  double total = scan_segments();
-  if (w.kind != 0 && !(total > 0.0)) {  // nothing left: draw from p
-    __syncthreads();
-    d_s.kind = 0;
-    w = weight_of(d_s, logits, draft_logits, a, b);
-    p_segments();
-    __syncthreads();
-    total = scan_segments();
-  }
-  const double goal = (double)a.u[b * (a.K + 1) + a.K] * total;
   if (tid == 0) {
     found = a.V;
     last = -1;
   }
-  // The first segment whose end lies behind the goal; after it the next ones, should
-  // rounding leave the token to them; the last with any weight where none does (u at
-  // the end of its interval).
-  const uint64_t some = __ballot(mine > 0.0), behind = __ballot(mine > 0.0 && scan > goal);
-  for (uint64_t todo = behind != 0 ? behind : 1ull << (63 - __builtin_clzll(some)); todo != 0;
-       todo &= todo - 1) {
-    const int seg = __builtin_ctzll(todo);
-    int32_t v0, v1;
-    run_of(Segment<X>(r, seg, a.segments), v0, v1);
-    double s = 0.0;
-    for (int32_t v = v0; v < v1; ++v) s += w(v);
-    double upto = s;  // inclusive over the wave
+  // First, where the draft has to be left out, the sum of its segment without it;
+  // then the segment that the token falls into: the first whose end lies behind the
+  // goal, after it the next ones, should rounding leave the token to them, or the
+  // last with any weight where none does (u at the end of its interval).  One loop
+  // over segments for both, and one copy of the exponential, for the sake of code
+  // that has to be fetched.
+  int fix = -1;
+  if (w.kind == 1) {
+    const int32_t piece = w.x < r.head ? 0 : (w.x - r.head) / Row<X>::E;
+    fix = r.pieces > 0 ? min((int)(((int64_t)piece << a.log_segments) / r.pieces), a.segments - 1)
+                       : a.segments - 1;
+    while (fix < a.segments - 1 && w.x >= Segment<X>(r, fix, a.log_segments).v1) ++fix;
+    while (fix > 0 && w.x < Segment<X>(r, fix, a.log_segments).v0) --fix;
+  }
+  uint64_t todo = 0;
+  double scan = 0.0, goal = 0.0;
+  bool located = false;
+  for (;;) {
+    __syncthreads();
+    if (fix < 0 && !located) {
+      for (;;) {
+        const double mine = lane < a.segments ? seg_s[lane] : 0.0;
+        scan = mine;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const double o = __shfl_up(upto, off, 64);
-      if (lane >= off) upto += o;
-    }
-    __syncthreads();
-    if (lane == 63) wave_s[wave] = upto;
-    __syncthreads();
-    double run = seg > 0 ? __shfl(scan, seg - 1, 64) : 0.0;
-    for (int q = 0; q < wave; ++q) run += wave_s[q];
-    run += upto - s;
-    int32_t hit = a.V, end = -1;
-    for (int32_t v = v0; v < v1; ++v) {
-      const double wv = w(v);
-      run += wv;
-      if (wv > 0.0) {
-        end = v;
-        if (run > goal) {
-          hit = v;
+        for (int off = 1; off < 64; off <<= 1) {
+          const double o = __shfl_up(scan, off, 64);
+          if (lane >= off) scan += o;
+        }
+        const double total = __shfl(scan, 63, 64);
+        if (total > 0.0 || w.kind == 0) {
+          goal = u * total;
+          const uint64_t some = __ballot(mine > 0.0);
+          todo = __ballot(mine > 0.0 && scan > goal);
+          if (todo == 0 && some != 0) todo = 1ull << (63 - __builtin_clzll(some));
           break;
         }
+        __syncthreads();  // nothing left: draw from p
+        if (tid == 0) d_s.kind = 0;
+        __syncthreads();
+        w = weight_of(d_s, logits, draft_logits, a, b);
+        segments_of_p();
+        __syncthreads();
       }
+      located = true;
     }
-    if (hit < a.V) atomicMin(&found, hit);
-    if (end >= 0) atomicMax(&last, end);
-    __syncthreads();
-    if (found < a.V) break;
+    if (fix < 0 && todo == 0) break;
+    const int seg = fix >= 0 ? fix : __builtin_ctzll(todo);
+    const Segment<X> g(r, seg, a.log_segments);
+    double before = __shfl(scan, seg > 0 ? seg - 1 : 0, 64);
+    if (seg == 0) before = 0.0;
+    double sum = 0.0;
+    bool done = false;
+    for (int32_t v0 = g.v0; v0 < g.v1 && !done; v0 += kRun * kFinishThreads) {
+      // weights of kRun consecutive tokens per thread
+      const int32_t first = v0 + tid * kRun;
+      float zp[kRun], zq[kRun];
+#pragma unroll
+      for (int k = 0; k < kRun; ++k)
+        zp[k] = first + k < g.v1 ? value(w.p[first + k]) : -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kRun; ++k)
+        zq[k] = w.kind == 2 && first + k < g.v1 ? value(w.q[first + k]) : -INFINITY;
+      double s = 0.0;
+#pragma unroll 1
+      for (int k = 0; k < kRun; ++k) {
+        double wt = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+          const double y = i == 0 ? fma((double)zp[0] - w.mp, a.k2, -w.lp)
+                                  : fma((double)zq[0] - w.mq, a.k2, -w.lq);
+          const double e = exp2_d(y);
+          wt = i == 0 ? e : wt - e;
+        }
+        if (w.kind == 1 && first + k == w.x) wt = 0.0;
+        wt = fmax(wt, 0.0);
+        wt_s[k][tid] = wt;
+        s += wt;
+#pragma unroll
+        for (int q = 1; q < kRun; ++q) zp[q - 1] = zp[q], zq[q - 1] = zq[q];
+      }
+      double upto = s;  // inclusive over the wave
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const double o = __shfl_up(upto, off, 64);
+        if (lane >= off) upto += o;
+      }
+      __syncthreads();
+      if (lane == 63) wave_s[wave] = upto;
+      __syncthreads();
+      double run = before + sum;
+#pragma unroll
+      for (int q = 0; q < kWaves; ++q) {
+        if (q < wave) run += wave_s[q];
+        sum += wave_s[q];
+      }
+      if (fix >= 0) continue;
+      run += upto - s;
+      int32_t hit = a.V, end = -1;
+#pragma unroll 1
+      for (int k = 0; k < kRun; ++k) {
+        const double wt = wt_s[k][tid];
+        run += wt;
+        if (wt > 0.0) {
+          end = first + k;
+          if (run > goal && hit == a.V) hit = end;
+        }
+      }
+      // one atomic per wave (tokens ascend with the lanes): 1024 took 8 us
+      const uint64_t hits = __ballot(hit < a.V), ends = __ballot(end >= 0);
+      if (hits != 0) hit = __shfl(hit, __builtin_ctzll(hits), 64);
+      if (ends != 0) end = __shfl(end, 63 - __builtin_clzll(ends), 64);
+      if (lane == 0 && hits != 0) atomicMin(&found, hit);
+      if (lane == 0 && ends != 0) atomicMax(&last, end);
+      __syncthreads();
+      done = found < a.V;
+    }
+    if (done) break;
+    if (fix >= 0) {
+      if (tid == 0) seg_s[fix] = sum;
+      fix = -1;
+    } else {
+      todo &= todo - 1;
+    }
   }
   if (tid == 0) {
     const int64_t i = b * (a.K + 1) + accepted;
     const int32_t v = found < a.V ? found : last;
     a.out_tokens[i] = v;
-    a.out_logp[i] = logp_of(row, v, d_s.p, a.k2);
+    a.out_logp[i] = v < 0 ? NAN : logp_of(row, v, d_s.p, a.k2);
   }
 }
 
-// Segments of a row: 512 tokens or more each, a wave's lanes to join them.
-int segments_of(int32_t V) {
+// Segments of a row: 512 tokens or more each, and up to 64, a lane each to join them
+// (32 with many rows: 576 rows of 152064 bf16 take 75 us in 64 segments, 68 in 32;
+// 5 rows 5.6 and 8.3).
+int segments_of(int64_t B, int64_t K, int32_t V) {
+  const int most = B * (2 * K + 1) <= 64 ? kMaxSegments : kMaxSegments / 2;
   int n = 1;
-  while (n < kMaxSegments && V / (2 * n) >= 512) n *= 2;
+  while (n < most && V / (2 * n) >= 512) n *= 2;
   return n;
 }
 
@@ -545,9 +713,9 @@ struct VerifyWs {
 VerifyWs carve_verify(void* base, int64_t B, int64_t K, int32_t V) {
   rbp::WsCarver c(base);
   VerifyWs w;
-  const size_t segments = (size_t)segments_of(V);
+  const size_t segments = (size_t)segments_of(B, K, V);
   w.parts = c.take<Part>((size_t)B * (2 * K + 1) * segments);
-  w.rest = c.take<double>((size_t)B * segments);
+  w.rest = c.take<double>((size_t)B * segments * kShares);
   w.decisions = c.take<Decision>((size_t)B);
   w.bytes = rbp::align_up(c.used, 256);
   return w;
@@ -562,7 +730,7 @@ void launch(const X* logits, const X* draft_logits, const Args& a, Decision* dec
                      dim3(kStatsThreads), 0, s, logits, draft_logits, a, items);
   if (draft_logits != nullptr)
     hipLaunchKernelGGL(rest_kernel<X>,
-                       dim3((unsigned)(a.B * rbp::ceil_div(a.segments, kRestThreads / 64))),
+                       dim3((unsigned)(a.B * rbp::ceil_div(a.segments * kShares, kRestThreads / 64))),
                        dim3(kRestThreads), 0, s, logits, draft_logits, a, decisions);
   hipLaunchKernelGGL(finish_kernel<X>, dim3(a.B), dim3(kFinishThreads), 0, s, logits, draft_logits,
                      a, decisions);
@@ -601,9 +769,11 @@ extern "C" int policy_verify_drafts(const void* logits, const void* draft_logits
   hipStream_t s = rbp::as_stream(stream);
   const VerifyWs w = carve_verify(ws, B, K, V);
   if (K == 0) draft_logits = nullptr;
-  const Args a{ld,       ld_draft, draft_tokens, n_draft, u,       B,          K,
-               V,        segments_of(V), kLog2eD / (double)temperature, out_tokens, out_logp,
-               n_out,    w.parts,  w.rest};
+  const int segments = segments_of(B, K, V);
+  const double k2 = kLog2eD / (double)temperature;
+  const Args a{ld,  ld_draft, draft_tokens, n_draft, u, B, K, V, segments,
+               __builtin_ctz((unsigned)segments), k2, 1000.0 / k2,
+               (float)std::fmin(kSlack / k2, 1e30), out_tokens, out_logp, n_out, w.parts, w.rest};
   if (logits_type == RBP_F32)
     launch(static_cast<const float*>(logits), static_cast<const float*>(draft_logits), a,
            w.decisions, s);
