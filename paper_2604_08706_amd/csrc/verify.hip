@@ -357,7 +357,7 @@ __device__ void decide(const X* __restrict__ logits, const X* __restrict__ draft
       out->q = rows_s[drawn_from_p || draft_logits == nullptr ? first : n + 1 + first];
       out->kind = !out->p.valid() ? -1
                   : drawn_from_p ? 0
-                  : draft_logits == nullptr ? 1
+                  : draft_logits == nullptr ? (out->x >= 0 && out->x < a.V ? 1 : 0)
                   : out->q.valid() ? 2 : 0;
     }
   }
@@ -575,6 +575,18 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
                        : a.segments - 1;
     while (fix < a.segments - 1 && w.x >= Segment<X>(r, fix, a.log_segments).v1) ++fix;
     while (fix > 0 && w.x < Segment<X>(r, fix, a.log_segments).v0) --fix;
+    // Taken off its segment's sum where that is exact enough: the two exponentials
+    // agree to 1e-13, so beside a remaining total of e / 8 or more the difference is
+    // off by less than 1e-12, and 2^-20 e is more than noise.
+    __syncthreads();
+    const double e = exp2_d(((double)value(w.p[w.x]) - w.mp) * a.k2);
+    const double left = seg_s[fix] - e;
+    const double rest = wave_sum(lane < a.segments ? seg_s[lane] : 0.0) - e;
+    __syncthreads();
+    if (left >= 0x1p-20 * e && rest >= 0.125 * e) {
+      if (tid == 0) seg_s[fix] = left;
+      fix = -1;
+    }
   }
   uint64_t todo = 0;
   double scan = 0.0, goal = 0.0;
@@ -660,7 +672,7 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
       if (fix >= 0) continue;
       run += upto - s;
       int32_t hit = a.V, end = -1;
-#pragma unroll 1
+#pragma unroll
       for (int k = 0; k < kRun; ++k) {
         const double wt = wt_s[k][tid];
         run += wt;
