@@ -24,41 +24,54 @@ using rbp::lp::pack_bf16x2;
 
 // ---- forward ------------------------------------------------------------------
 
-// One 16-byte piece of a row per thread.
+constexpr int kRowPieces = 4;  // 16-byte pieces of a thread, their loads in flight together
+
+// Pieces of rows by a block: kRowPieces times 256 consecutive ones.
 __global__ void __launch_bounds__(256) embed_kernel(const uint16_t* __restrict__ table,
                                                     const int32_t* __restrict__ tokens,
                                                     const int32_t* __restrict__ seq, int64_t n,
-                                                    int32_t d8, int32_t V, float scale,
+                                                    uint32_t d8, int32_t V, float scale,
                                                     uint4* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  const int64_t t = i / d8;
-  const int32_t c = (int32_t)(i - t * d8);
-  uint4 o = make_uint4(0u, 0u, 0u, 0u);
-  if (seq == nullptr || seq[t] >= 0) {
-    const int32_t y = tokens[t];
-    if (y >= 0 && y < V) {
-      const uint4 w = reinterpret_cast<const uint4*>(table)[(int64_t)y * d8 + c];
-      const uint32_t a[4] = {w.x, w.y, w.z, w.w};
-      uint32_t r[4];
+  const int64_t first = (int64_t)blockIdx.x * (256 * kRowPieces);
+  // row and piece of the block's first piece; the others are less than 2^31 behind it
+  const int64_t t0 = first / d8;
+  const uint32_t c0 = (uint32_t)(first - t0 * d8);
+  uint4 w[kRowPieces];
+  bool zero[kRowPieces], bad[kRowPieces];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        r[k] = pack_bf16x2(scale * bf16_to_f32((uint16_t)(a[k] & 0xffff)),
-                           scale * bf16_to_f32((uint16_t)(a[k] >> 16)));
-      o = make_uint4(r[0], r[1], r[2], r[3]);
-    } else {
-      o = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
-    }
+  for (int k = 0; k < kRowPieces; ++k) {
+    const uint32_t i = k * 256 + threadIdx.x, at = c0 + i;
+    zero[k] = bad[k] = false;
+    w[k] = make_uint4(0u, 0u, 0u, 0u);
+    if (first + i >= n) continue;
+    const int64_t t = t0 + at / d8;
+    const int32_t y = tokens[t];
+    zero[k] = seq != nullptr && seq[t] < 0;
+    bad[k] = !(y >= 0 && y < V);
+    if (!zero[k] && !bad[k])
+      w[k] = reinterpret_cast<const uint4*>(table)[(int64_t)y * d8 + at % d8];
   }
-  out[i] = o;
+#pragma unroll
+  for (int k = 0; k < kRowPieces; ++k) {
+    const int64_t i = first + k * 256 + threadIdx.x;
+    if (i >= n) continue;
+    const uint32_t a[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      r[j] = pack_bf16x2(scale * bf16_to_f32((uint16_t)(a[j] & 0xffff)),
+                         scale * bf16_to_f32((uint16_t)(a[j] >> 16)));
+    const bool nan = bad[k] && !zero[k];
+    out[i] = nan       ? make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u)
+             : zero[k] ? make_uint4(0u, 0u, 0u, 0u)
+                       : make_uint4(r[0], r[1], r[2], r[3]);
+  }
 }
 
 // ---- sorting the tokens ---------------------------------------------------------
 
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kItems = 8;  // keys per thread
-constexpr int kTile = kSortThreads * kItems;
 constexpr int kMaxDigit = 9;
 constexpr int kBins = 1 << kMaxDigit;
 static_assert(kBins == kSortThreads, "one bin per thread");
@@ -69,75 +82,41 @@ __device__ __forceinline__ uint32_t key_of(const int32_t* __restrict__ tokens,
   const int32_t y = tokens[t];
   return (seq == nullptr || seq[t] >= 0) && y >= 0 && y < V ? (uint32_t)y : (uint32_t)V;
 }
-
-// Keys of a pass: the tokens' in the first, the previous pass's output later.
-struct Keys {
-  const int32_t *tokens, *seq;
-  const uint32_t *key, *at;
-  int32_t V;
-  __device__ __forceinline__ uint32_t load(int64_t i) const {
-    return key == nullptr ? key_of(tokens, seq, i, V) : key[i];
-  }
-  __device__ __forceinline__ uint32_t position(int64_t i) const {
-    return key == nullptr ? (uint32_t)i : at[i];
-  }
-};
-
-// hist[block][digit]: the keys of the block's tile by digit.
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Keys in, int64_t T, int shift,
-                                                                  uint32_t* __restrict__ hist) {
-  __shared__ uint32_t bins[kBins];
-  bins[threadIdx.x] = 0;
-  __syncthreads();
-  const int64_t t0 = (int64_t)blockIdx.x * kTile;
-#pragma unroll
-  for (int k = 0; k < kItems; ++k) {
-    const int64_t i = t0 + k * kSortThreads + threadIdx.x;
-    if (i < T) atomicAdd(&bins[(in.load(i) >> shift) & (kBins - 1)], 1u);
-  }
-  __syncthreads();
-  hist[(int64_t)blockIdx.x * kBins + threadIdx.x] = bins[threadIdx.x];
+__device__ __forceinline__ uint32_t digit_of(uint32_t key, int shift) {
+  return (key >> shift) & (kBins - 1);
 }
 
-// One pass: every key of the tile to its place, keys of equal digits in order.
-// A wave takes 512 consecutive keys, 64 at a time; lanes with the same digit find
-// each other by ballots over its bits, and the wave's counts so far give their
-// ranks.
-__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
-    Keys in, int64_t T, int shift, const uint32_t* __restrict__ hist, int n_tiles,
-    uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out) {
-  __shared__ uint32_t cnt[kSortWaves][kBins];
-  __shared__ uint32_t base[kBins], wave_sum[kSortWaves];
+// dW's rows are cleared by blocks behind those of the sort's launches, so that the
+// sort, which keeps few units busy, costs next to nothing beside it.
+struct Fill {
+  float4* p;
+  int64_t n;
+  int blocks;  // of this launch, behind the sort's
+};
+__device__ __forceinline__ void fill(const Fill& f, int block) {
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int64_t i = (int64_t)block * kSortThreads + threadIdx.x; i < f.n;
+       i += (int64_t)f.blocks * kSortThreads)
+    f.p[i] = zero;
+}
+
+// Ranks of a tile's keys by digit, in order: a wave takes kItems * 64 consecutive
+// keys, 64 at a time; lanes with the same digit find each other by ballots over its
+// bits, and the wave's counts so far give their ranks.  place[k] is the key's rank
+// among the wave's keys of its digit; cnt[wave][digit] ends up as the number of them
+// in the waves before.
+template <int kItems>
+__device__ __forceinline__ void rank_tile(const uint32_t (&key)[kItems], int live_items,
+                                          int shift, uint32_t (*cnt)[kBins],
+                                          uint32_t (&place)[kItems]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
   for (int w = 0; w < kSortWaves; ++w) cnt[w][tid] = 0;
-  // this thread's bin: keys of it in all tiles, and in those before this one
-  uint32_t total = 0, before = 0;
-  for (int b = 0; b < n_tiles; ++b) {
-    const uint32_t h = hist[(int64_t)b * kBins + tid];
-    total += h;
-    if (b < (int)blockIdx.x) before += h;
-  }
-  uint32_t scan = total;  // inclusive over the bins
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t o = __shfl_up(scan, off, 64);
-    if (lane >= off) scan += o;
-  }
-  if (lane == 63) wave_sum[wave] = scan;
   __syncthreads();
-  uint32_t lower = scan - total;
-  for (int w = 0; w < wave; ++w) lower += wave_sum[w];
-  base[tid] = lower + before;
-
-  const int64_t t0 = (int64_t)blockIdx.x * kTile + wave * (64 * kItems);
-  uint32_t key[kItems], place[kItems];
 #pragma unroll
   for (int k = 0; k < kItems; ++k) {
-    const int64_t i = t0 + k * 64 + lane;
-    const bool live = i < T;
-    key[k] = live ? in.load(i) : 0u;
-    const uint32_t digit = (key[k] >> shift) & (kBins - 1);
+    const bool live = k * 64 + lane < live_items;
+    const uint32_t digit = digit_of(key[k], shift);
     uint64_t same = __ballot(live);
 #pragma unroll
     for (int bit = 0; bit < kMaxDigit; ++bit) {
@@ -161,25 +140,167 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
     run += c;
   }
   __syncthreads();
+}
+
+// Exclusive sum over the bins, one per thread.
+__device__ __forceinline__ uint32_t scan_bins(uint32_t total, uint32_t* wave_sum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t scan = total;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(scan, off, 64);
+    if (lane >= off) scan += o;
+  }
+  if (lane == 63) wave_sum[wave] = scan;
+  __syncthreads();
+  uint32_t lower = scan - total;
+#pragma unroll
+  for (int w = 0; w < kSortWaves - 1; ++w)
+    if (w < wave) lower += wave_sum[w];
+  return lower;
+}
+
+// Up to kSortThreads * kItems tokens, in one block: every pass in LDS.
+template <int kItems>
+__global__ void __launch_bounds__(kSortThreads) sort_one_kernel(
+    const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int32_t T,
+    int passes, uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
+  constexpr int kTile = kSortThreads * kItems;
+  __shared__ uint32_t cnt[kSortWaves][kBins], base[kBins], wave_sum[kSortWaves];
+  __shared__ uint32_t key_s[kTile];
+  __shared__ uint16_t at_s[kTile];
+  if (blockIdx.x > 0) return fill(f, blockIdx.x - 1);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int i0 = wave * (64 * kItems) + lane, live = T - wave * (64 * kItems);
+  uint32_t key[kItems], at[kItems], place[kItems];
+#pragma unroll
+  for (int k = 0; k < kItems; ++k) {
+    at[k] = i0 + k * 64;
+    key[k] = (int)at[k] < T ? key_of(tokens, seq, at[k], V) : 0u;
+  }
+  for (int p = 0;; ++p) {
+    const int shift = p * kMaxDigit;
+    rank_tile<kItems>(key, live, shift, cnt, place);
+    // (cnt[last wave][bin] + its own keys: the bin's total, from the keys' last ranks)
+    base[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kItems; ++k)
+      if (i0 + k * 64 < T) atomicAdd(&base[digit_of(key[k], shift)], 1u);
+    __syncthreads();
+    const uint32_t lower = scan_bins(base[tid], wave_sum);
+    __syncthreads();
+    base[tid] = lower;
+    __syncthreads();
+    const bool last = p == passes - 1;
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      if (i0 + k * 64 >= T) continue;
+      const uint32_t digit = digit_of(key[k], shift);
+      const uint32_t to = base[digit] + cnt[wave][digit] + place[k];
+      if (last) {
+        key_out[to] = key[k];
+        at_out[to] = at[k];
+      } else {
+        key_s[to] = key[k];
+        at_s[to] = (uint16_t)at[k];
+      }
+    }
+    if (last) return;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kItems; ++k)
+      if (i0 + k * 64 < T) {
+        key[k] = key_s[i0 + k * 64];
+        at[k] = at_s[i0 + k * 64];
+      }
+    __syncthreads();
+  }
+}
+
+// hist[tile][digit] of the first pass, and zeros for the second pass's.
+template <int kItems>
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(
+    const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int64_t T,
+    int n_tiles, uint32_t* __restrict__ hist, uint32_t* __restrict__ next_hist, Fill f) {
+  __shared__ uint32_t bins[kBins];
+  if ((int)blockIdx.x >= n_tiles) return fill(f, blockIdx.x - n_tiles);
+  bins[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * (kSortThreads * kItems);
+#pragma unroll
+  for (int k = 0; k < kItems; ++k) {
+    const int64_t i = t0 + k * kSortThreads + threadIdx.x;
+    if (i < T) atomicAdd(&bins[digit_of(key_of(tokens, seq, i, V), 0)], 1u);
+  }
+  __syncthreads();
+  const int64_t o = (int64_t)blockIdx.x * kBins + threadIdx.x;
+  hist[o] = bins[threadIdx.x];
+  next_hist[o] = 0;
+}
+
+// Keys of a pass: the tokens' in the first, the previous pass's output later.
+struct Keys {
+  const int32_t *tokens, *seq;
+  const uint32_t *key, *at;
+  int32_t V;
+};
+
+// One pass: every key of the tile to its place.  The next pass's tiles are counted
+// where the keys go (integers: the order does not matter); the pass after that gets
+// its zeros.
+template <int kItems>
+__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
+    Keys in, int64_t T, int shift, const uint32_t* __restrict__ hist,
+    uint32_t* __restrict__ next_hist, uint32_t* __restrict__ after_hist, int n_tiles,
+    uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
+  constexpr int kTile = kSortThreads * kItems;
+  __shared__ uint32_t cnt[kSortWaves][kBins];
+  __shared__ uint32_t base[kBins], wave_sum[kSortWaves];
+  if ((int)blockIdx.x >= n_tiles) return fill(f, blockIdx.x - n_tiles);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t t0 = (int64_t)blockIdx.x * kTile + wave * (64 * kItems);
+  const int live = T - t0 < kTile ? (int)(T - t0) : kTile;
+  uint32_t key[kItems], at[kItems], place[kItems];
 #pragma unroll
   for (int k = 0; k < kItems; ++k) {
     const int64_t i = t0 + k * 64 + lane;
-    if (i >= T) continue;
-    const uint32_t digit = (key[k] >> shift) & (kBins - 1);
+    key[k] = i >= T ? 0u : in.key == nullptr ? key_of(in.tokens, in.seq, i, in.V) : in.key[i];
+    at[k] = i >= T || in.key == nullptr ? (uint32_t)i : in.at[i];
+  }
+  // this thread's bin: keys of it in all tiles, and in those before this one
+  uint32_t total = 0, before = 0;
+#pragma unroll 8
+  for (int b = 0; b < n_tiles; ++b) {
+    const uint32_t h = hist[(int64_t)b * kBins + tid];
+    total += h;
+    before += b < (int)blockIdx.x ? h : 0u;
+  }
+  base[tid] = scan_bins(total, wave_sum) + before;
+  if (after_hist != nullptr) after_hist[(int64_t)blockIdx.x * kBins + tid] = 0;
+  rank_tile<kItems>(key, live, shift, cnt, place);
+#pragma unroll
+  for (int k = 0; k < kItems; ++k) {
+    if (k * 64 + lane >= live) continue;
+    const uint32_t digit = digit_of(key[k], shift);
     const uint32_t to = base[digit] + cnt[wave][digit] + place[k];
     key_out[to] = key[k];
-    at_out[to] = in.position(i);
+    at_out[to] = at[k];
+    if (next_hist != nullptr)
+      atomicAdd(&next_hist[(int64_t)(to / kTile) * kBins + digit_of(key[k], shift + kMaxDigit)],
+                1u);
   }
 }
 
 // ---- sums over runs -------------------------------------------------------------
 
 constexpr uint32_t kNoKey = 0xffffffffu;
-constexpr int kSlice = 32;  // sorted positions per slice
 
 struct Sorted {
   const uint32_t *key, *at;
   int64_t T;
+  int32_t slice;     // positions per slice, a power of two
+  int64_t n_slices;
   __device__ __forceinline__ uint32_t key_at(int64_t i) const {
     return i >= 0 && i < T ? key[i] : kNoKey;
   }
@@ -208,109 +329,144 @@ __device__ __forceinline__ void store8(float* __restrict__ p, const Row8& r) {
   reinterpret_cast<float4*>(p)[0] = make_float4(r.v[0], r.v[1], r.v[2], r.v[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(r.v[4], r.v[5], r.v[6], r.v[7]);
 }
-
-// dW's 8 columns at p: scale sum, added to what is there or in its place.
-__device__ __forceinline__ void put8(float* __restrict__ p, const Row8& sum, float scale,
-                                     bool accumulate) {
-  Row8 o{};
-  if (accumulate) o = load8(static_cast<const float*>(p));
+__device__ __forceinline__ void add8(Row8& a, const Row8& b) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) o.v[k] = fmaf(scale, sum.v[k], o.v[k]);
-  store8(p, o);
+  for (int k = 0; k < 8; ++k) a.v[k] += b.v[k];
 }
+// old + scale sum
+__device__ __forceinline__ Row8 scaled(const Row8& old, const Row8& sum, float scale) {
+  Row8 o;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) o.v[k] = fmaf(scale, sum.v[k], old.v[k]);
+  return o;
+}
+
+constexpr int kBatch = 4;  // rows of dx, and of dW, in flight
 
 // A group of kLanes lanes (8 columns each) per slice and kLanes * 8 columns.
 // part[slice][0]: the sum of the run that came in from the slice before,
 // part[slice][1]: of the run that begins here and goes on behind it.
-template <class X, int kLanes>
+template <class X, int kLanes, bool kAdd>
 __global__ void __launch_bounds__(256) run_sum_kernel(const X* __restrict__ dx, Sorted in,
-                                                      int64_t n_slices, int n_chunks, int32_t d,
-                                                      int32_t V, float scale, int accumulate,
-                                                      float* __restrict__ dW,
+                                                      int n_chunks, int32_t d, int32_t V,
+                                                      float scale, float* __restrict__ dW,
                                                       float* __restrict__ part) {
   const int64_t g = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
   const int64_t slice = g / n_chunks;
-  const int32_t col = ((int32_t)(g % n_chunks) * kLanes + (int)(threadIdx.x % kLanes)) * 8;
-  if (slice >= n_slices || col >= d) return;
-  const int64_t i0 = slice * kSlice, i1 = i0 + kSlice < in.T ? i0 + kSlice : in.T;
-  uint32_t cur = in.key_at(i0);
-  bool begins = cur != in.key_at(i0 - 1);
+  const int q = threadIdx.x % kLanes;
+  const int32_t col = ((int32_t)(g % n_chunks) * kLanes + q) * 8;
+  if (slice >= in.n_slices) return;  // whole groups
+  const bool live = col < d;
+  const int64_t i0 = slice * in.slice, i1 = i0 + in.slice < in.T ? i0 + in.slice : in.T;
+  bool begins = in.key_at(i0 - 1) != in.key[i0], open = false;
   Row8 acc{};
-  auto flush = [&](bool ends) {
-    if (cur >= (uint32_t)V) return;
-    if (begins && ends)
-      put8(dW + (int64_t)cur * d + col, acc, scale, accumulate != 0);
-    else
-      store8(part + (slice * 2 + (begins ? 1 : 0)) * d + col, acc);
-  };
-  for (int64_t i = i0; i < i1; ++i) {
-    const uint32_t k = in.key[i];
-    if (k != cur) {
-      flush(true);
-      cur = k;
-      begins = true;
-      acc = Row8{};
-    }
-    if (k >= (uint32_t)V) break;
-    const Row8 r = load8(dx + (int64_t)in.at[i] * d + col);
+  for (int64_t base = i0; base < i1; base += kLanes) {
+    // a lane per position: its key, its row, and whether its run ends there
+    const int64_t mine = base + q;
+    const uint32_t key = mine < i1 ? in.key[mine] : kNoKey;
+    const uint32_t at = mine < i1 ? in.at[mine] : 0u;
+    const bool end = key != in.key_at(mine + 1);
+    const int here = i1 - base < kLanes ? (int)(i1 - base) : kLanes;
+    for (int j0 = 0; j0 < here; j0 += kBatch) {
+      Row8 row[kBatch], old[kBatch];
+      uint32_t k[kBatch];
+      bool ends[kBatch];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) acc.v[q] += r.v[q];
+      for (int j = 0; j < kBatch; ++j) {
+        // (kLanes is a multiple of kBatch: the lane exists)
+        k[j] = __shfl(key, j0 + j, kLanes);
+        ends[j] = __shfl((int)end, j0 + j, kLanes) != 0;
+        const uint32_t t = __shfl(at, j0 + j, kLanes);
+        row[j] = Row8{};
+        old[j] = Row8{};
+        if (!live || k[j] >= (uint32_t)V) continue;
+        row[j] = load8(dx + (int64_t)t * d + col);
+        if (kAdd && ends[j]) old[j] = load8(static_cast<const float*>(dW) + (int64_t)k[j] * d + col);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (!live || k[j] >= (uint32_t)V) continue;
+        add8(acc, row[j]);
+        open = !ends[j];
+        if (!ends[j]) continue;
+        if (begins)
+          store8(dW + (int64_t)k[j] * d + col, scaled(old[j], acc, scale));
+        else
+          store8(part + slice * 2 * d + col, acc);
+        acc = Row8{};
+        begins = true;
+      }
+    }
   }
-  flush(cur != in.key_at(i1));
+  if (open) store8(part + (slice * 2 + (begins ? 1 : 0)) * d + col, acc);
 }
 
 // The runs that cross slices, by the slice they begin in.
-template <int kLanes>
-__global__ void __launch_bounds__(256) run_join_kernel(Sorted in, int64_t n_slices, int n_chunks,
-                                                       int32_t d, int32_t V, float scale,
-                                                       int accumulate, float* __restrict__ dW,
+template <int kLanes, bool kAdd>
+__global__ void __launch_bounds__(256) run_join_kernel(Sorted in, int n_chunks, int32_t d,
+                                                       int32_t V, float scale,
+                                                       float* __restrict__ dW,
                                                        const float* __restrict__ part) {
   const int64_t g = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
   const int64_t slice = g / n_chunks;
-  const int32_t col = ((int32_t)(g % n_chunks) * kLanes + (int)(threadIdx.x % kLanes)) * 8;
-  if (slice >= n_slices || col >= d) return;
-  const int64_t i0 = slice * kSlice, i1 = i0 + kSlice;
+  const int q = threadIdx.x % kLanes;
+  const int32_t col = ((int32_t)(g % n_chunks) * kLanes + q) * 8;
+  if (slice >= in.n_slices) return;
+  const int64_t i0 = slice * in.slice, i1 = i0 + in.slice;
   if (i1 >= in.T) return;
-  const uint32_t cur = in.key[i1 - 1];
-  if (cur >= (uint32_t)V || in.key[i1] != cur) return;
-  if (in.key[i0] == cur && in.key_at(i0 - 1) == cur) return;  // began before
-  Row8 acc = load8(part + (slice * 2 + 1) * d + col);
-  for (int64_t j = slice + 1;; ++j) {
-    const Row8 r = load8(part + j * 2 * d + col);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) acc.v[q] += r.v[q];
-    const int64_t end = (j + 1) * kSlice;  // behind slice j
-    if (end >= in.T || in.key[end] != cur) break;
+  const uint32_t cur = in.key[i1 - 1], next = in.key[i1], first = in.key[i0],
+                 prev = in.key_at(i0 - 1);
+  if (cur >= (uint32_t)V || next != cur) return;
+  if (first == cur && prev == cur) return;  // began before
+  // slices behind this one that the run reaches into, a lane each
+  int64_t more = 0;
+  for (;;) {
+    const bool goes_on = in.key_at(i1 + (more + q + 1) * in.slice) == cur;
+    const uint64_t all = __ballot(goes_on) >> ((threadIdx.x & 63) / kLanes * kLanes);
+    const int n = all == ~0ull ? 64 : __builtin_ctzll(~all);
+    if (n < kLanes) {
+      more += n + 1;
+      break;
+    }
+    more += kLanes;
   }
-  put8(dW + (int64_t)cur * d + col, acc, scale, accumulate != 0);
+  if (col >= d) return;
+  Row8 acc = load8(part + (slice * 2 + 1) * d + col);
+  const float* p = part + (slice + 1) * 2 * d + col;
+  constexpr int kJoin = 8;
+  for (int64_t j = 0; j < more; j += kJoin) {
+    Row8 r[kJoin];
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i)
+      if (j + i < more) r[i] = load8(p + (j + i) * 2 * d);
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i)
+      if (j + i < more) add8(acc, r[i]);
+  }
+  float* o = dW + (int64_t)cur * d + col;
+  store8(o, scaled(kAdd ? load8(static_cast<const float*>(o)) : Row8{}, acc, scale));
 }
 
-__global__ void __launch_bounds__(256) zero_kernel(float4* __restrict__ p, int64_t n) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
-    p[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+__global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill(f, blockIdx.x); }
+
+// Keys per thread of a sort's tile: small tiles while their counts, which every tile
+// reads, stay few.
+inline int sort_items(int64_t T) { return T <= 65536 ? 2 : 8; }
+constexpr int kOneItems = 8;  // keys per thread where one block sorts all
+
+// Positions per slice: enough slices to fill the chip (a group of lanes each, and
+// chunk of columns), few enough that a run over many slices is joined soon.
+inline int32_t slice_of(int64_t T, int n_chunks) {
+  int32_t s = 8;
+  while (s < 256 && T * n_chunks > (int64_t)s * 4096) s *= 2;
+  return s;
 }
 
 struct EmbedWs {
-  uint32_t *key[2], *at[2], *hist;
+  uint32_t *key[2], *at[2], *hist[3];
   float* part;
   size_t bytes;
 };
-
-EmbedWs carve_embed(void* base, int64_t T, int32_t d) {
-  rbp::WsCarver c(base);
-  const size_t n = (size_t)T;
-  EmbedWs w;
-  for (int k = 0; k < 2; ++k) {
-    w.key[k] = c.take<uint32_t>(n);
-    w.at[k] = c.take<uint32_t>(n);
-  }
-  w.hist = c.take<uint32_t>((size_t)rbp::ceil_div(T, kTile) * kBins);
-  w.part = c.take<float>((size_t)rbp::ceil_div(T, kSlice) * 2 * (size_t)d);
-  w.bytes = rbp::align_up(c.used, 256);
-  return w;
-}
-
-inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 template <class Launch>
 void with_lanes(int32_t d8, Launch&& launch) {
@@ -323,6 +479,32 @@ void with_lanes(int32_t d8, Launch&& launch) {
   else
     launch(std::integral_constant<int, 64>{});
 }
+
+int chunks_of(int32_t d) {
+  int n = 1;
+  with_lanes(d / 8, [&](auto lanes) {
+    n = (int)rbp::ceil_div(d / 8, decltype(lanes)::value);
+  });
+  return n;
+}
+
+EmbedWs carve_embed(void* base, int64_t T, int32_t d) {
+  rbp::WsCarver c(base);
+  const size_t n = (size_t)T;
+  EmbedWs w;
+  for (int k = 0; k < 2; ++k) {
+    w.key[k] = c.take<uint32_t>(n);
+    w.at[k] = c.take<uint32_t>(n);
+  }
+  const size_t tiles = (size_t)rbp::ceil_div(T, kSortThreads * sort_items(T));
+  for (int k = 0; k < 3; ++k) w.hist[k] = c.take<uint32_t>(tiles * kBins);
+  const int32_t dd = d < 8 ? 8 : d;
+  w.part = c.take<float>((size_t)rbp::ceil_div(T, slice_of(T, chunks_of(dd))) * 2 * (size_t)dd);
+  w.bytes = rbp::align_up(c.used, 256);
+  return w;
+}
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 }  // namespace
 
@@ -344,11 +526,10 @@ extern "C" int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
   RBP_REQUIRE(table && tokens && out, RBP_EINVAL, "policy_embed_fwd: null pointer");
   RBP_REQUIRE(aligned(table, 16) && aligned(out, 16), RBP_EUNSUPPORTED,
               "policy_embed_fwd: table and out must be aligned to 16 bytes");
-  const int64_t n = T * (d / 8);
-  RBP_REQUIRE(rbp::ceil_div(n, 256) <= INT32_MAX, RBP_EUNSUPPORTED,
-              "policy_embed_fwd: T * d too large");
-  hipLaunchKernelGGL(embed_kernel, dim3((unsigned)rbp::ceil_div(n, 256)), dim3(256), 0,
-                     rbp::as_stream(stream), table, tokens, seq_of_token, n, d / 8, V, scale,
+  const int64_t n = T * (d / 8), blocks = rbp::ceil_div(n, 256 * kRowPieces);
+  RBP_REQUIRE(blocks <= INT32_MAX, RBP_EUNSUPPORTED, "policy_embed_fwd: T * d too large");
+  hipLaunchKernelGGL(embed_kernel, dim3((unsigned)blocks), dim3(256), 0, rbp::as_stream(stream),
+                     table, tokens, seq_of_token, n, (uint32_t)(d / 8), V, scale,
                      reinterpret_cast<uint4*>(out));
   RBP_CHECK_LAUNCH("policy_embed_fwd");
   return RBP_OK;
@@ -373,45 +554,87 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   RBP_REQUIRE(T == 0 || (ws && ws_bytes >= need), RBP_EWORKSPACE,
               "policy_embed_bwd: workspace needs %zu bytes, got %zu", need, ws_bytes);
   hipStream_t s = rbp::as_stream(stream);
-  if (!accumulate_dW) {
-    const int64_t n = (int64_t)V * (d / 4), blocks = rbp::ceil_div(n, 256 * 4);
-    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0,
-                       s, reinterpret_cast<float4*>(dW), n);
-    RBP_CHECK_LAUNCH("policy_embed_bwd");
-  }
-  if (T == 0) return RBP_OK;
-  const EmbedWs w = carve_embed(ws, T, d);
-  const int n_tiles = (int)rbp::ceil_div(T, kTile);
   int bits = 1;
   while (bits < 31 && (V >> bits) != 0) ++bits;  // keys go up to V
   const int passes = (bits + kMaxDigit - 1) / kMaxDigit;
-  Keys in{tokens, seq_of_token, nullptr, nullptr, V};
-  for (int p = 0; p < passes; ++p) {
-    const int shift = p * kMaxDigit;
-    hipLaunchKernelGGL(sort_count_kernel, dim3(n_tiles), dim3(kSortThreads), 0, s, in, T, shift,
-                       w.hist);
-    hipLaunchKernelGGL(sort_scatter_kernel, dim3(n_tiles), dim3(kSortThreads), 0, s, in, T, shift,
-                       w.hist, n_tiles, w.key[p & 1], w.at[p & 1]);
-    in.key = w.key[p & 1];
-    in.at = w.at[p & 1];
+  const bool one = T <= kSortThreads * kOneItems;
+  // dW's rows to be cleared, in equal shares behind each launch of the sort
+  const int64_t n_fill = accumulate_dW ? 0 : (int64_t)V * (d / 4);
+  const int n_launches = T == 0 || one ? 1 : passes + 1;
+  int launch = 0;
+  auto share = [&] {
+    const int64_t from = n_fill * launch / n_launches, to = n_fill * (launch + 1) / n_launches;
+    ++launch;
+    const int64_t blocks = rbp::ceil_div(to - from, kSortThreads * 4);
+    return Fill{reinterpret_cast<float4*>(dW) + from, to - from,
+                (int)(blocks < 4096 ? blocks : 4096)};
+  };
+  if (T == 0) {
+    const Fill f = share();
+    if (f.blocks > 0) hipLaunchKernelGGL(zero_kernel, dim3(f.blocks), dim3(kSortThreads), 0, s, f);
+    RBP_CHECK_LAUNCH("policy_embed_bwd");
+    return RBP_OK;
+  }
+  const EmbedWs w = carve_embed(ws, T, d);
+  const uint32_t *key = w.key[0], *at = w.at[0];
+  if (one) {
+    const Fill f = share();
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(1 + f.blocks), dim3(kSortThreads), 0, s, tokens, seq_of_token,
+                         V, (int32_t)T, passes, w.key[0], w.at[0], f);
+    };
+    if (T <= kSortThreads)
+      go(sort_one_kernel<1>);
+    else if (T <= kSortThreads * 2)
+      go(sort_one_kernel<2>);
+    else
+      go(sort_one_kernel<kOneItems>);
+  } else {
+    auto go = [&](auto items) {
+      constexpr int kItems = decltype(items)::value;
+      const int n_tiles = (int)rbp::ceil_div(T, kSortThreads * kItems);
+      Fill f = share();
+      hipLaunchKernelGGL(sort_count_kernel<kItems>, dim3(n_tiles + f.blocks), dim3(kSortThreads), 0,
+                         s, tokens, seq_of_token, V, T, n_tiles, w.hist[0], w.hist[1], f);
+      Keys in{tokens, seq_of_token, nullptr, nullptr, V};
+      for (int p = 0; p < passes; ++p) {
+        f = share();
+        hipLaunchKernelGGL(sort_scatter_kernel<kItems>, dim3(n_tiles + f.blocks),
+                           dim3(kSortThreads), 0, s, in, T, p * kMaxDigit, w.hist[p % 3],
+                           p + 1 < passes ? w.hist[(p + 1) % 3] : nullptr,
+                           p + 2 < passes ? w.hist[(p + 2) % 3] : nullptr, n_tiles, w.key[p & 1],
+                           w.at[p & 1], f);
+        in.key = key = w.key[p & 1];
+        in.at = at = w.at[p & 1];
+      }
+    };
+    if (sort_items(T) == 2)
+      go(std::integral_constant<int, 2>{});
+    else
+      go(std::integral_constant<int, 8>{});
   }
   RBP_CHECK_LAUNCH("policy_embed_bwd");
-  const Sorted sorted{in.key, in.at, T};
-  const int64_t n_slices = rbp::ceil_div(T, kSlice);
   with_lanes(d / 8, [&](auto lanes) {
     constexpr int kLanes = decltype(lanes)::value;
     const int n_chunks = (int)rbp::ceil_div(d / 8, kLanes);
-    const dim3 grid((unsigned)rbp::ceil_div(n_slices * n_chunks * kLanes, 256));
-    if (dx_type == RBP_F32)
-      hipLaunchKernelGGL((run_sum_kernel<float, kLanes>), grid, dim3(256), 0, s,
-                         static_cast<const float*>(dx), sorted, n_slices, n_chunks, d, V, scale,
-                         accumulate_dW, dW, w.part);
+    const int32_t slice = slice_of(T, n_chunks);
+    const Sorted sorted{key, at, T, slice, rbp::ceil_div(T, slice)};
+    const dim3 grid((unsigned)rbp::ceil_div(sorted.n_slices * n_chunks * kLanes, 256));
+    auto go = [&](auto sum, auto join, auto* x) {
+      hipLaunchKernelGGL(sum, grid, dim3(256), 0, s, x, sorted, n_chunks, d, V, scale, dW, w.part);
+      hipLaunchKernelGGL(join, grid, dim3(256), 0, s, sorted, n_chunks, d, V, scale, dW,
+                         (const float*)w.part);
+    };
+    const auto* x32 = static_cast<const float*>(dx);
+    const auto* x16 = static_cast<const uint16_t*>(dx);
+    if (dx_type == RBP_F32 && accumulate_dW)
+      go(run_sum_kernel<float, kLanes, true>, run_join_kernel<kLanes, true>, x32);
+    else if (dx_type == RBP_F32)
+      go(run_sum_kernel<float, kLanes, false>, run_join_kernel<kLanes, false>, x32);
+    else if (accumulate_dW)
+      go(run_sum_kernel<uint16_t, kLanes, true>, run_join_kernel<kLanes, true>, x16);
     else
-      hipLaunchKernelGGL((run_sum_kernel<uint16_t, kLanes>), grid, dim3(256), 0, s,
-                         static_cast<const uint16_t*>(dx), sorted, n_slices, n_chunks, d, V, scale,
-                         accumulate_dW, dW, w.part);
-    hipLaunchKernelGGL(run_join_kernel<kLanes>, grid, dim3(256), 0, s, sorted, n_slices, n_chunks,
-                       d, V, scale, accumulate_dW, dW, w.part);
+      go(run_sum_kernel<uint16_t, kLanes, false>, run_join_kernel<kLanes, false>, x16);
   });
   RBP_CHECK_LAUNCH("policy_embed_bwd");
   return RBP_OK;
