@@ -26,7 +26,10 @@ using rbp::lp::pack_bf16x2;
 
 constexpr int kRowPieces = 4;  // 16-byte pieces of a thread, their loads in flight together
 
-// Pieces of rows by a block: kRowPieces times 256 consecutive ones.
+// Pieces of rows by a block: kRowPieces times 256 consecutive ones.  Large outputs
+// are stored past the caches (kBypass), which then keep the rows that tokens share:
+// 16384 x 3584 43.7 -> 35.5 us (4.7 TB/s), 16384 x 896 11.5 -> 9.0.
+template <bool kBypass>
 __global__ void __launch_bounds__(256) embed_kernel(const uint16_t* __restrict__ table,
                                                     const int32_t* __restrict__ tokens,
                                                     const int32_t* __restrict__ seq, int64_t n,
@@ -62,16 +65,21 @@ __global__ void __launch_bounds__(256) embed_kernel(const uint16_t* __restrict__
       r[j] = pack_bf16x2(scale * bf16_to_f32((uint16_t)(a[j] & 0xffff)),
                          scale * bf16_to_f32((uint16_t)(a[j] >> 16)));
     const bool nan = bad[k] && !zero[k];
-    out[i] = nan       ? make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u)
-             : zero[k] ? make_uint4(0u, 0u, 0u, 0u)
-                       : make_uint4(r[0], r[1], r[2], r[3]);
+    const uint4 o = nan       ? make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u)
+                    : zero[k] ? make_uint4(0u, 0u, 0u, 0u)
+                              : make_uint4(r[0], r[1], r[2], r[3]);
+    if constexpr (kBypass) {
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, o), reinterpret_cast<u32x4*>(out + i));
+    } else {
+      out[i] = o;
+    }
   }
 }
 
 // ---- sorting the tokens ---------------------------------------------------------
 
 constexpr int kSortThreads = 512;
-constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kMaxDigit = 9;
 constexpr int kBins = 1 << kMaxDigit;
 static_assert(kBins == kSortThreads, "one bin per thread");
@@ -93,10 +101,11 @@ struct Fill {
   int64_t n;
   int blocks;  // of this launch, behind the sort's
 };
+template <int kThreads>
 __device__ __forceinline__ void fill(const Fill& f, int block) {
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int64_t i = (int64_t)block * kSortThreads + threadIdx.x; i < f.n;
-       i += (int64_t)f.blocks * kSortThreads)
+  for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < f.n;
+       i += (int64_t)f.blocks * kThreads)
     f.p[i] = zero;
 }
 
@@ -104,14 +113,13 @@ __device__ __forceinline__ void fill(const Fill& f, int block) {
 // keys, 64 at a time; lanes with the same digit find each other by ballots over its
 // bits, and the wave's counts so far give their ranks.  place[k] is the key's rank
 // among the wave's keys of its digit; cnt[wave][digit] ends up as the number of them
-// in the waves before.
-template <int kItems>
+// in the waves before, cnt[kWaves][digit] as that of the tile.
+template <int kItems, int kWaves>
 __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kItems], int live_items,
                                           int shift, uint32_t (*cnt)[kBins],
                                           uint32_t (&place)[kItems]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-#pragma unroll
-  for (int w = 0; w < kSortWaves; ++w) cnt[w][tid] = 0;
+  for (int i = tid; i < kWaves * kBins; i += kWaves * 64) cnt[0][i] = 0;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kItems; ++k) {
@@ -132,18 +140,22 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kItems], int liv
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
-  uint32_t run = 0;
+  if (tid < kBins) {
+    uint32_t run = 0;
 #pragma unroll
-  for (int w = 0; w < kSortWaves; ++w) {
-    const uint32_t c = cnt[w][tid];
-    cnt[w][tid] = run;
-    run += c;
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t c = cnt[w][tid];
+      cnt[w][tid] = run;
+      run += c;
+    }
+    cnt[kWaves][tid] = run;
   }
   __syncthreads();
 }
 
-// Exclusive sum over the bins, one per thread.
+// Exclusive sum over the bins, one per thread (threads behind them bring 0).
 __device__ __forceinline__ uint32_t scan_bins(uint32_t total, uint32_t* wave_sum) {
+  constexpr int kBinWaves = kBins / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t scan = total;
 #pragma unroll
@@ -151,25 +163,26 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t total, uint32_t* wave_sum
     const uint32_t o = __shfl_up(scan, off, 64);
     if (lane >= off) scan += o;
   }
-  if (lane == 63) wave_sum[wave] = scan;
+  if (lane == 63 && wave < kBinWaves) wave_sum[wave] = scan;
   __syncthreads();
   uint32_t lower = scan - total;
 #pragma unroll
-  for (int w = 0; w < kSortWaves - 1; ++w)
+  for (int w = 0; w < kBinWaves - 1; ++w)
     if (w < wave) lower += wave_sum[w];
   return lower;
 }
 
-// Up to kSortThreads * kItems tokens, in one block: every pass in LDS.
-template <int kItems>
-__global__ void __launch_bounds__(kSortThreads) sort_one_kernel(
+// Up to kThreads * kItems tokens, in one block: every pass in LDS.
+template <int kThreads, int kItems>
+__global__ void __launch_bounds__(kThreads) sort_one_kernel(
     const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int32_t T,
     int passes, uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
-  constexpr int kTile = kSortThreads * kItems;
-  __shared__ uint32_t cnt[kSortWaves][kBins], base[kBins], wave_sum[kSortWaves];
+  constexpr int kTile = kThreads * kItems, kWaves = kThreads / 64;
+  static_assert(kTile <= 65536 && kThreads >= kBins, "16-bit positions, a bin per thread");
+  __shared__ uint32_t cnt[kWaves + 1][kBins], base[kBins], wave_sum[kBins / 64];
   __shared__ uint32_t key_s[kTile];
   __shared__ uint16_t at_s[kTile];
-  if (blockIdx.x > 0) return fill(f, blockIdx.x - 1);
+  if (blockIdx.x > 0) return fill<kThreads>(f, blockIdx.x - 1);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i0 = wave * (64 * kItems) + lane, live = T - wave * (64 * kItems);
   uint32_t key[kItems], at[kItems], place[kItems];
@@ -180,17 +193,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_one_kernel(
   }
   for (int p = 0;; ++p) {
     const int shift = p * kMaxDigit;
-    rank_tile<kItems>(key, live, shift, cnt, place);
-    // (cnt[last wave][bin] + its own keys: the bin's total, from the keys' last ranks)
-    base[tid] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kItems; ++k)
-      if (i0 + k * 64 < T) atomicAdd(&base[digit_of(key[k], shift)], 1u);
-    __syncthreads();
-    const uint32_t lower = scan_bins(base[tid], wave_sum);
-    __syncthreads();
-    base[tid] = lower;
+    rank_tile<kItems, kWaves>(key, live, shift, cnt, place);
+    const uint32_t lower = scan_bins(tid < kBins ? cnt[kWaves][tid] : 0u, wave_sum);
+    if (tid < kBins) base[tid] = lower;
     __syncthreads();
     const bool last = p == passes - 1;
 #pragma unroll
@@ -214,29 +219,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_one_kernel(
         key[k] = key_s[i0 + k * 64];
         at[k] = at_s[i0 + k * 64];
       }
-    __syncthreads();
   }
-}
-
-// hist[tile][digit] of the first pass, and zeros for the second pass's.
-template <int kItems>
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(
-    const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int64_t T,
-    int n_tiles, uint32_t* __restrict__ hist, uint32_t* __restrict__ next_hist, Fill f) {
-  __shared__ uint32_t bins[kBins];
-  if ((int)blockIdx.x >= n_tiles) return fill(f, blockIdx.x - n_tiles);
-  bins[threadIdx.x] = 0;
-  __syncthreads();
-  const int64_t t0 = (int64_t)blockIdx.x * (kSortThreads * kItems);
-#pragma unroll
-  for (int k = 0; k < kItems; ++k) {
-    const int64_t i = t0 + k * kSortThreads + threadIdx.x;
-    if (i < T) atomicAdd(&bins[digit_of(key_of(tokens, seq, i, V), 0)], 1u);
-  }
-  __syncthreads();
-  const int64_t o = (int64_t)blockIdx.x * kBins + threadIdx.x;
-  hist[o] = bins[threadIdx.x];
-  next_hist[o] = 0;
 }
 
 // Keys of a pass: the tokens' in the first, the previous pass's output later.
@@ -244,20 +227,41 @@ struct Keys {
   const int32_t *tokens, *seq;
   const uint32_t *key, *at;
   int32_t V;
+  __device__ __forceinline__ uint32_t load(int64_t i) const {
+    return key == nullptr ? key_of(tokens, seq, i, V) : key[i];
+  }
 };
 
-// One pass: every key of the tile to its place.  The next pass's tiles are counted
-// where the keys go (integers: the order does not matter); the pass after that gets
-// its zeros.
+// hist[tile][digit] of a pass.  (Counted by atomics where the pass before puts its
+// keys instead, a frequent token's take turns: 8 us more there, 4.6 for this launch.)
+template <int kItems>
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Keys in, int64_t T, int shift,
+                                                                  int n_tiles,
+                                                                  uint32_t* __restrict__ hist,
+                                                                  Fill f) {
+  __shared__ uint32_t bins[kBins];
+  if ((int)blockIdx.x >= n_tiles) return fill<kSortThreads>(f, blockIdx.x - n_tiles);
+  bins[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * (kSortThreads * kItems);
+#pragma unroll
+  for (int k = 0; k < kItems; ++k) {
+    const int64_t i = t0 + k * kSortThreads + threadIdx.x;
+    if (i < T) atomicAdd(&bins[digit_of(in.load(i), shift)], 1u);
+  }
+  __syncthreads();
+  hist[(int64_t)blockIdx.x * kBins + threadIdx.x] = bins[threadIdx.x];
+}
+
+// One pass: every key of the tile to its place.
 template <int kItems>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
-    Keys in, int64_t T, int shift, const uint32_t* __restrict__ hist,
-    uint32_t* __restrict__ next_hist, uint32_t* __restrict__ after_hist, int n_tiles,
+    Keys in, int64_t T, int shift, const uint32_t* __restrict__ hist, int n_tiles,
     uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
-  constexpr int kTile = kSortThreads * kItems;
-  __shared__ uint32_t cnt[kSortWaves][kBins];
-  __shared__ uint32_t base[kBins], wave_sum[kSortWaves];
-  if ((int)blockIdx.x >= n_tiles) return fill(f, blockIdx.x - n_tiles);
+  constexpr int kTile = kSortThreads * kItems, kWaves = kSortThreads / 64;
+  __shared__ uint32_t cnt[kWaves + 1][kBins];
+  __shared__ uint32_t base[kBins], wave_sum[kBins / 64];
+  if ((int)blockIdx.x >= n_tiles) return fill<kSortThreads>(f, blockIdx.x - n_tiles);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t0 = (int64_t)blockIdx.x * kTile + wave * (64 * kItems);
   const int live = T - t0 < kTile ? (int)(T - t0) : kTile;
@@ -265,7 +269,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
 #pragma unroll
   for (int k = 0; k < kItems; ++k) {
     const int64_t i = t0 + k * 64 + lane;
-    key[k] = i >= T ? 0u : in.key == nullptr ? key_of(in.tokens, in.seq, i, in.V) : in.key[i];
+    key[k] = i >= T ? 0u : in.load(i);
     at[k] = i >= T || in.key == nullptr ? (uint32_t)i : in.at[i];
   }
   // this thread's bin: keys of it in all tiles, and in those before this one
@@ -277,8 +281,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
     before += b < (int)blockIdx.x ? h : 0u;
   }
   base[tid] = scan_bins(total, wave_sum) + before;
-  if (after_hist != nullptr) after_hist[(int64_t)blockIdx.x * kBins + tid] = 0;
-  rank_tile<kItems>(key, live, shift, cnt, place);
+  rank_tile<kItems, kWaves>(key, live, shift, cnt, place);
 #pragma unroll
   for (int k = 0; k < kItems; ++k) {
     if (k * 64 + lane >= live) continue;
@@ -286,9 +289,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
     const uint32_t to = base[digit] + cnt[wave][digit] + place[k];
     key_out[to] = key[k];
     at_out[to] = at[k];
-    if (next_hist != nullptr)
-      atomicAdd(&next_hist[(int64_t)(to / kTile) * kBins + digit_of(key[k], shift + kMaxDigit)],
-                1u);
   }
 }
 
@@ -401,58 +401,71 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const X* __restrict__ dx, 
   if (open) store8(part + (slice * 2 + (begins ? 1 : 0)) * d + col, acc);
 }
 
-// The runs that cross slices, by the slice they begin in.
+// The runs that cross slices, by a block for each slice that one begins in and chunk
+// of columns: its groups of lanes take equal stretches of the run's slices, and
+// the first adds their sums.
 template <int kLanes, bool kAdd>
 __global__ void __launch_bounds__(256) run_join_kernel(Sorted in, int n_chunks, int32_t d,
                                                        int32_t V, float scale,
                                                        float* __restrict__ dW,
                                                        const float* __restrict__ part) {
-  const int64_t g = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
-  const int64_t slice = g / n_chunks;
-  const int q = threadIdx.x % kLanes;
-  const int32_t col = ((int32_t)(g % n_chunks) * kLanes + q) * 8;
-  if (slice >= in.n_slices) return;
+  constexpr int kGroups = 256 / kLanes, kJoin = 4;
+  __shared__ Row8 sum_s[kGroups][kLanes];
+  const int64_t slice = blockIdx.x / n_chunks;
+  const int q = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  const int32_t col = ((int32_t)(blockIdx.x % n_chunks) * kLanes + q) * 8;
   const int64_t i0 = slice * in.slice, i1 = i0 + in.slice;
   if (i1 >= in.T) return;
   const uint32_t cur = in.key[i1 - 1], next = in.key[i1], first = in.key[i0],
                  prev = in.key_at(i0 - 1);
   if (cur >= (uint32_t)V || next != cur) return;
   if (first == cur && prev == cur) return;  // began before
-  // slices behind this one that the run reaches into, a lane each
-  int64_t more = 0;
+  // slices behind this one that the run reaches into, tried 64 at a time by each wave
+  int64_t more = 1;
   for (;;) {
-    const bool goes_on = in.key_at(i1 + (more + q + 1) * in.slice) == cur;
-    const uint64_t all = __ballot(goes_on) >> ((threadIdx.x & 63) / kLanes * kLanes);
-    const int n = all == ~0ull ? 64 : __builtin_ctzll(~all);
-    if (n < kLanes) {
-      more += n + 1;
+    const int lane = threadIdx.x & 63;
+    const uint64_t on = __ballot(in.key_at(i1 + (more + lane) * in.slice) == cur);
+    if (on != ~0ull) {
+      more += __builtin_ctzll(~on);
       break;
     }
-    more += kLanes;
+    more += 64;
   }
-  if (col >= d) return;
-  Row8 acc = load8(part + (slice * 2 + 1) * d + col);
-  const float* p = part + (slice + 1) * 2 * d + col;
-  constexpr int kJoin = 8;
-  for (int64_t j = 0; j < more; j += kJoin) {
-    Row8 r[kJoin];
+  const bool live = col < d;
+  Row8 acc{};
+  if (live) {
+    const float* p = part + (slice + 1) * 2 * d + col;
+    const int64_t from = more * group / kGroups, to = more * (group + 1) / kGroups;
+    if (group == 0) acc = load8(part + (slice * 2 + 1) * d + col);
+    for (int64_t j = from; j < to; j += kJoin) {
+      Row8 r[kJoin];
 #pragma unroll
-    for (int i = 0; i < kJoin; ++i)
-      if (j + i < more) r[i] = load8(p + (j + i) * 2 * d);
+      for (int i = 0; i < kJoin; ++i)
+        if (j + i < to) r[i] = load8(p + (j + i) * 2 * d);
 #pragma unroll
-    for (int i = 0; i < kJoin; ++i)
-      if (j + i < more) add8(acc, r[i]);
+      for (int i = 0; i < kJoin; ++i)
+        if (j + i < to) add8(acc, r[i]);
+    }
   }
+  sum_s[group][q] = acc;
+  __syncthreads();
+  if (group != 0 || !live) return;
+  for (int g = 1; g < kGroups; ++g) add8(acc, sum_s[g][q]);
   float* o = dW + (int64_t)cur * d + col;
   store8(o, scaled(kAdd ? load8(static_cast<const float*>(o)) : Row8{}, acc, scale));
 }
 
-__global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill(f, blockIdx.x); }
+__global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill<kSortThreads>(f, blockIdx.x); }
 
 // Keys per thread of a sort's tile: small tiles while their counts, which every tile
 // reads, stay few.
 inline int sort_items(int64_t T) { return T <= 65536 ? 2 : 8; }
-constexpr int kOneItems = 8;  // keys per thread where one block sorts all
+// Tokens that one block sorts: 6144, or 16384 beside the clearing of much of dW.  By
+// itself it takes 45 us for 16384, tiles on many units 19 in four launches; behind
+// 545 MB to be cleared (92 us) the one launch is the better (117 us in all against
+// 134).
+constexpr int kOneMost = 6144, kOneBeside = 16384;
+constexpr int64_t kBesideFill = 1 << 24;  // float4 of dW
 
 // Positions per slice: enough slices to fill the chip (a group of lanes each, and
 // chunk of columns), few enough that a run over many slices is joined soon.
@@ -463,7 +476,7 @@ inline int32_t slice_of(int64_t T, int n_chunks) {
 }
 
 struct EmbedWs {
-  uint32_t *key[2], *at[2], *hist[3];
+  uint32_t *key[2], *at[2], *hist;
   float* part;
   size_t bytes;
 };
@@ -497,7 +510,7 @@ EmbedWs carve_embed(void* base, int64_t T, int32_t d) {
     w.at[k] = c.take<uint32_t>(n);
   }
   const size_t tiles = (size_t)rbp::ceil_div(T, kSortThreads * sort_items(T));
-  for (int k = 0; k < 3; ++k) w.hist[k] = c.take<uint32_t>(tiles * kBins);
+  w.hist = c.take<uint32_t>(tiles * kBins);
   const int32_t dd = d < 8 ? 8 : d;
   w.part = c.take<float>((size_t)rbp::ceil_div(T, slice_of(T, chunks_of(dd))) * 2 * (size_t)dd);
   w.bytes = rbp::align_up(c.used, 256);
@@ -528,9 +541,8 @@ extern "C" int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
               "policy_embed_fwd: table and out must be aligned to 16 bytes");
   const int64_t n = T * (d / 8), blocks = rbp::ceil_div(n, 256 * kRowPieces);
   RBP_REQUIRE(blocks <= INT32_MAX, RBP_EUNSUPPORTED, "policy_embed_fwd: T * d too large");
-  hipLaunchKernelGGL(embed_kernel, dim3((unsigned)blocks), dim3(256), 0, rbp::as_stream(stream),
-                     table, tokens, seq_of_token, n, (uint32_t)(d / 8), V, scale,
-                     reinterpret_cast<uint4*>(out));
+  hipLaunchKernelGGL(n >= (1 << 19) ? embed_kernel<true> : embed_kernel<false>,
+                     dim3((unsigned)blocks), dim3(256), 0, rbp::as_stream(stream), table, tokens, seq_of_token, n, (uint32_t)(d / 8), V, scale, reinterpret_cast<uint4*>(out));
   RBP_CHECK_LAUNCH("policy_embed_fwd");
   return RBP_OK;
 }
@@ -557,21 +569,23 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   int bits = 1;
   while (bits < 31 && (V >> bits) != 0) ++bits;  // keys go up to V
   const int passes = (bits + kMaxDigit - 1) / kMaxDigit;
-  const bool one = T <= kSortThreads * kOneItems;
   // dW's rows to be cleared, in equal shares behind each launch of the sort
   const int64_t n_fill = accumulate_dW ? 0 : (int64_t)V * (d / 4);
-  const int n_launches = T == 0 || one ? 1 : passes + 1;
+  const bool one = T <= kOneMost || (T <= kOneBeside && n_fill >= kBesideFill);
+  const int n_launches = T == 0 || one ? 1 : 2 * passes;
   int launch = 0;
   auto share = [&] {
     const int64_t from = n_fill * launch / n_launches, to = n_fill * (launch + 1) / n_launches;
     ++launch;
+    // (a few stores a thread: 545 MB 93 us with 4096 blocks, 86 so)
     const int64_t blocks = rbp::ceil_div(to - from, kSortThreads * 4);
     return Fill{reinterpret_cast<float4*>(dW) + from, to - from,
-                (int)(blocks < 4096 ? blocks : 4096)};
+                (int)(blocks < (1 << 28) ? blocks : (1 << 28))};
   };
   if (T == 0) {
     const Fill f = share();
-    if (f.blocks > 0) hipLaunchKernelGGL(zero_kernel, dim3(f.blocks), dim3(kSortThreads), 0, s, f);
+    if (f.blocks == 0) return RBP_OK;
+    hipLaunchKernelGGL(zero_kernel, dim3(f.blocks), dim3(kSortThreads), 0, s, f);
     RBP_CHECK_LAUNCH("policy_embed_bwd");
     return RBP_OK;
   }
@@ -579,30 +593,33 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   const uint32_t *key = w.key[0], *at = w.at[0];
   if (one) {
     const Fill f = share();
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3(1 + f.blocks), dim3(kSortThreads), 0, s, tokens, seq_of_token,
-                         V, (int32_t)T, passes, w.key[0], w.at[0], f);
+    auto go = [&](auto threads, auto items) {
+      constexpr int kThreads = decltype(threads)::value, kItems = decltype(items)::value;
+      hipLaunchKernelGGL((sort_one_kernel<kThreads, kItems>), dim3(1 + f.blocks), dim3(kThreads), 0,
+                         s, tokens, seq_of_token, V, (int32_t)T, passes, w.key[0], w.at[0], f);
     };
-    if (T <= kSortThreads)
-      go(sort_one_kernel<1>);
-    else if (T <= kSortThreads * 2)
-      go(sort_one_kernel<2>);
+    using std::integral_constant;
+    if (T <= 512)
+      go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+    else if (T <= 2048)
+      go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    else if (T <= 6144)
+      go(integral_constant<int, 1024>{}, integral_constant<int, 6>{});
     else
-      go(sort_one_kernel<kOneItems>);
+      go(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
   } else {
     auto go = [&](auto items) {
       constexpr int kItems = decltype(items)::value;
       const int n_tiles = (int)rbp::ceil_div(T, kSortThreads * kItems);
-      Fill f = share();
-      hipLaunchKernelGGL(sort_count_kernel<kItems>, dim3(n_tiles + f.blocks), dim3(kSortThreads), 0,
-                         s, tokens, seq_of_token, V, T, n_tiles, w.hist[0], w.hist[1], f);
       Keys in{tokens, seq_of_token, nullptr, nullptr, V};
       for (int p = 0; p < passes; ++p) {
+        const int shift = p * kMaxDigit;
+        Fill f = share();
+        hipLaunchKernelGGL(sort_count_kernel<kItems>, dim3(n_tiles + f.blocks), dim3(kSortThreads),
+                           0, s, in, T, shift, n_tiles, w.hist, f);
         f = share();
         hipLaunchKernelGGL(sort_scatter_kernel<kItems>, dim3(n_tiles + f.blocks),
-                           dim3(kSortThreads), 0, s, in, T, p * kMaxDigit, w.hist[p % 3],
-                           p + 1 < passes ? w.hist[(p + 1) % 3] : nullptr,
-                           p + 2 < passes ? w.hist[(p + 2) % 3] : nullptr, n_tiles, w.key[p & 1],
+                           dim3(kSortThreads), 0, s, in, T, shift, w.hist, n_tiles, w.key[p & 1],
                            w.at[p & 1], f);
         in.key = key = w.key[p & 1];
         in.at = at = w.at[p & 1];
@@ -622,8 +639,8 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
     const dim3 grid((unsigned)rbp::ceil_div(sorted.n_slices * n_chunks * kLanes, 256));
     auto go = [&](auto sum, auto join, auto* x) {
       hipLaunchKernelGGL(sum, grid, dim3(256), 0, s, x, sorted, n_chunks, d, V, scale, dW, w.part);
-      hipLaunchKernelGGL(join, grid, dim3(256), 0, s, sorted, n_chunks, d, V, scale, dW,
-                         (const float*)w.part);
+      hipLaunchKernelGGL(join, dim3((unsigned)(sorted.n_slices * n_chunks)), dim3(256), 0, s,
+                         sorted, n_chunks, d, V, scale, dW, (const float*)w.part);
     };
     const auto* x32 = static_cast<const float*>(dx);
     const auto* x16 = static_cast<const uint16_t*>(dx);
