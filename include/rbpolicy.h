@@ -562,8 +562,8 @@ int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
  *         with a tied head, the dW of policy_logprob_bwd or policy_fused_fwd_bwd.
  * ws      device, >= rbp_workspace_bytes(RBP_OP_EMBED_BWD, T, d, V).
  * Errors: RBP_EINVAL (null pointers, T < 0, d < 1, V < 1, an unknown dx_type, scale
- *         not finite); RBP_EUNSUPPORTED (d % 8 != 0, dx or dW not aligned to 16
- *         bytes, T above 2^30); RBP_EWORKSPACE.
+ *         not finite, ws not aligned to 16 bytes); RBP_EUNSUPPORTED (d % 8 != 0, dx
+ *         or dW not aligned to 16 bytes, T above 2^30); RBP_EWORKSPACE.
  */
 int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
                      const int32_t* seq_of_token, int64_t T, int32_t d, int32_t V,
@@ -605,9 +605,9 @@ int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
  * is drawn from p_a.
  * ws      device, >= rbp_workspace_bytes(RBP_OP_VERIFY, B, K, V).
  * Errors: RBP_EINVAL (null pointers, B < 0, K < 0, V < 1, ld or ld_draft < V, an
- *         unknown type, temperature not positive and finite, logits not aligned
- *         to their type); RBP_EUNSUPPORTED (K above 255, B (K + 1) above 2^24);
- *         RBP_EWORKSPACE.
+ *         unknown type, temperature outside [2^-100, 2^100], logits not aligned to
+ *         their type or ws to 16 bytes); RBP_EUNSUPPORTED (K above 255, B (K + 1)
+ *         above 2^24); RBP_EWORKSPACE.
  */
 int policy_verify_drafts(const void* logits, const void* draft_logits, int logits_type,
                          int64_t ld, int64_t ld_draft, const int32_t* draft_tokens,
@@ -644,8 +644,8 @@ int policy_verify_drafts(const void* logits, const void* draft_logits, int logit
  *         in columns [0, V) of every row; may be `logits` itself.
  * ws      device, >= rbp_workspace_bytes(RBP_OP_DISTILL, T, K, V).
  * Errors: RBP_EINVAL (null pointers, T < 0, V < 1, K < 1, ld < V, B < 1, n_seq_total
- *         < 1, an unknown type, temperature not positive and finite, scale not
- *         finite, logits or dlogits not aligned to their type);
+ *         < 1, an unknown type, temperature outside [2^-100, 2^100], scale not
+ *         finite, logits or dlogits not aligned to their type or ws to 16 bytes);
  *         RBP_EUNSUPPORTED (K above 256, T above 2^31 - 1); RBP_EWORKSPACE.
  */
 int policy_distill_fwd_bwd(const void* logits, int logits_type, int64_t ld,

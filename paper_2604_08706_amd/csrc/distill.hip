@@ -621,8 +621,9 @@ extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64
               "policy_distill_fwd_bwd: need B >= 1 and n_seq_total >= 1");
   RBP_REQUIRE(logits_type == RBP_BF16 || logits_type == RBP_F32, RBP_EINVAL,
               "policy_distill_fwd_bwd: unknown logits_type %d", logits_type);
-  RBP_REQUIRE(std::isfinite(temperature) && temperature > 0.0f && std::isfinite(scale), RBP_EINVAL,
-              "policy_distill_fwd_bwd: need a positive temperature and a finite scale");
+  RBP_REQUIRE(temperature >= 0x1p-100f && temperature <= 0x1p100f && std::isfinite(scale),
+              RBP_EINVAL, "policy_distill_fwd_bwd: need a temperature in [2^-100, 2^100] and a "
+              "finite scale");
   RBP_REQUIRE(K <= kMaxK, RBP_EUNSUPPORTED, "policy_distill_fwd_bwd: K above %d", kMaxK);
   RBP_REQUIRE(T <= INT32_MAX, RBP_EUNSUPPORTED, "policy_distill_fwd_bwd: T above 2^31 - 1");
   RBP_REQUIRE(loss_accum && stats && seq_len, RBP_EINVAL, "policy_distill_fwd_bwd: null pointer");
@@ -630,8 +631,9 @@ extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64
   RBP_REQUIRE(logits && teacher_ids && teacher_logits && seq_of_token && kl, RBP_EINVAL,
               "policy_distill_fwd_bwd: null per-token pointer");
   const size_t es = logits_type == RBP_F32 ? 4 : 2;
-  RBP_REQUIRE(aligned(logits, es) && aligned(dlogits, es), RBP_EINVAL,
-              "policy_distill_fwd_bwd: logits or dlogits not aligned to their type");
+  RBP_REQUIRE(aligned(logits, es) && aligned(dlogits, es) && aligned(ws, 16), RBP_EINVAL,
+              "policy_distill_fwd_bwd: logits or dlogits not aligned to their type, or ws to 16 "
+              "bytes");
   const size_t need = rbp::distill_ws(T, K, V);
   RBP_REQUIRE(ws && ws_bytes >= need, RBP_EWORKSPACE,
               "policy_distill_fwd_bwd: workspace needs %zu bytes, got %zu", need, ws_bytes);

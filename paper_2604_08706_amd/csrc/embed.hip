@@ -460,11 +460,11 @@ __global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill<kSort
 // Keys per thread of a sort's tile: small tiles while their counts, which every tile
 // reads, stay few.
 inline int sort_items(int64_t T) { return T <= 65536 ? 2 : 8; }
-// Tokens that one block sorts: 6144, or 16384 beside the clearing of much of dW.  By
+// Tokens that one block sorts: 6144, or 12288 beside the clearing of much of dW.  By
 // itself it takes 45 us for 16384, tiles on many units 19 in four launches; behind
-// 545 MB to be cleared (92 us) the one launch is the better (117 us in all against
-// 134).
-constexpr int kOneMost = 6144, kOneBeside = 16384;
+// 545 MB to be cleared (86 us) the one launch is the better (10007 tokens 114 us in
+// all against 134).
+constexpr int kOneMost = 6144, kOneBeside = 12288;
 constexpr int64_t kBesideFill = 1 << 24;  // float4 of dW
 
 // Positions per slice: enough slices to fill the chip (a group of lanes each, and
@@ -562,6 +562,7 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   RBP_REQUIRE(dW && (T == 0 || (dx && tokens)), RBP_EINVAL, "policy_embed_bwd: null pointer");
   RBP_REQUIRE(aligned(dW, 16) && aligned(dx, 16), RBP_EUNSUPPORTED,
               "policy_embed_bwd: dx and dW must be aligned to 16 bytes");
+  RBP_REQUIRE(aligned(ws, 16), RBP_EINVAL, "policy_embed_bwd: ws must be aligned to 16 bytes");
   const size_t need = T == 0 ? 0 : rbp::embed_bwd_ws(T, d, V);
   RBP_REQUIRE(T == 0 || (ws && ws_bytes >= need), RBP_EWORKSPACE,
               "policy_embed_bwd: workspace needs %zu bytes, got %zu", need, ws_bytes);
@@ -606,7 +607,7 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
     else if (T <= 6144)
       go(integral_constant<int, 1024>{}, integral_constant<int, 6>{});
     else
-      go(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+      go(integral_constant<int, 1024>{}, integral_constant<int, 12>{});
   } else {
     auto go = [&](auto items) {
       constexpr int kItems = decltype(items)::value;

@@ -765,16 +765,16 @@ extern "C" int policy_verify_drafts(const void* logits, const void* draft_logits
               RBP_EINVAL, "policy_verify_drafts: need B >= 0, K >= 0, V >= 1, ld and ld_draft >= V");
   RBP_REQUIRE(logits_type == RBP_BF16 || logits_type == RBP_F32, RBP_EINVAL,
               "policy_verify_drafts: unknown logits_type %d", logits_type);
-  RBP_REQUIRE(std::isfinite(temperature) && temperature > 0.0f, RBP_EINVAL,
-              "policy_verify_drafts: temperature must be positive and finite");
+  RBP_REQUIRE(temperature >= 0x1p-100f && temperature <= 0x1p100f, RBP_EINVAL,
+              "policy_verify_drafts: temperature must lie in [2^-100, 2^100]");
   RBP_REQUIRE(K <= 255 && (int64_t)B * (K + 1) <= (1 << 24), RBP_EUNSUPPORTED,
               "policy_verify_drafts: K above 255 or B (K + 1) above 2^24");
   if (B == 0) return RBP_OK;
   RBP_REQUIRE(logits && u && out_tokens && out_logp && n_out && (K == 0 || draft_tokens),
               RBP_EINVAL, "policy_verify_drafts: null pointer");
   const size_t es = logits_type == RBP_F32 ? 4 : 2;
-  RBP_REQUIRE(aligned(logits, es) && aligned(draft_logits, es), RBP_EINVAL,
-              "policy_verify_drafts: logits not aligned to their type");
+  RBP_REQUIRE(aligned(logits, es) && aligned(draft_logits, es) && aligned(ws, 16), RBP_EINVAL,
+              "policy_verify_drafts: logits not aligned to their type, or ws to 16 bytes");
   const size_t need = rbp::verify_ws(B, K, V);
   RBP_REQUIRE(ws && ws_bytes >= need, RBP_EWORKSPACE,
               "policy_verify_drafts: workspace needs %zu bytes, got %zu", need, ws_bytes);

@@ -122,7 +122,8 @@ def _run(rbp, z, ids, lt, mass, seq, seq_len, tau=1.0, scale=1.0, dtype=torch.fl
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("T,V,K", [(1, 1, 1), (1, 7, 3), (37, 1024, 8), (5, 1000, 256), (9, 63, 64),
-                                   (3, 4097, 17), (2, 20000, 5), (33, 513, 65), (4, 33333, 100)])
+                                   (3, 4097, 17), (2, 20000, 5), (33, 513, 65), (4, 33333, 100),
+                                   (40, 40001, 9), (64, 8191, 3), (16, 8192, 2)])
 def test_divergence_and_gradient(T, V, K, dtype):
     rbp = require_gpu()
     a = _case(T, V, K, dtype, T + V + K)[:6]
@@ -201,25 +202,55 @@ def test_absent_entries_and_empty_rows():
         _run(rbp, z, ids, lt, None, seq, seq_len, dtype=dtype, grad=None)
 
 
-def test_infinite_divergence_and_invalid_values():
+@pytest.mark.parametrize("V", [300, 20000])
+def test_infinite_divergence_and_invalid_values(V):
     """p > 0 where the policy has no mass: KL = inf and a finite gradient; NaN logits, ids behind
     the vocabulary: NaN."""
     rbp = require_gpu()
-    z, ids, lt, _, seq, seq_len, _ = _case(5, 300, 4, torch.float32, 50)
+    z, ids, lt, _, seq, seq_len, _ = _case(5, V, 4, torch.float32, 50)
     seq[:] = 0
     z[0, ids[0, 0]] = -np.inf
     z[1, 17] = np.nan
-    ids[2, 1] = 300
+    ids[2, 1] = V
     ids[3, 2] = 2 ** 31 - 1
     lt[4, 0] = np.nan
     kl, loss, stats = (torch.zeros(n, device="cuda") for n in (5, 1, 2))
-    dz = torch.zeros((5, 300), device="cuda")
+    dz = torch.zeros((5, V), device="cuda")
     rbp.policy_distill_fwd_bwd(_cuda(z).float(), _cuda(ids), _cuda(lt), None, _cuda(seq),
                                _cuda(seq_len), 1, kl, loss, stats, dz,
-                               rbp.workspace(rbp.RBP_OP_DISTILL, 5, 4, 300))
+                               rbp.workspace(rbp.RBP_OP_DISTILL, 5, 4, V))
     assert kl[0].item() == np.inf and kl[1:].isnan().all()
     assert dz[0].isfinite().all() and dz[2].isfinite().all() and dz[3].isfinite().all()
     assert dz[1].isnan().all() and dz[4].isnan().all() and loss.isnan().all()
+
+
+@pytest.mark.parametrize("V", [901, 3001, 8001, 30001, 60001])
+def test_large_passes_give_the_rows_of_small_ones(V):
+    """Beyond 3/4 GiB the gradient is stored otherwise: the same bits."""
+    rbp = require_gpu()
+    a = _case(50, V, 5, torch.bfloat16, V)[:6]
+    z, ids, lt, _, seq, seq_len = a
+    times = (3 << 28) // (50 * V * 2) + 1
+
+    def call(n):
+        T = 50 * n
+        zt = _cuda(z).bfloat16().repeat(n, 1)
+        dz, kl = torch.empty_like(zt), torch.empty(T, device="cuda")
+        loss, stats = torch.zeros(1, device="cuda"), torch.zeros(2, device="cuda")
+        rbp.policy_distill_fwd_bwd(zt, _cuda(ids).repeat(n, 1), _cuda(lt).repeat(n, 1), None,
+                                   _cuda(seq).repeat(n), _cuda(seq_len), 9, kl, loss, stats, dz,
+                                   rbp.workspace(rbp.RBP_OP_DISTILL, T, 5, V))
+        return kl.view(n, 50), dz.view(n, 50, V), stats
+
+    print(f"[distill] {times} times 50 rows of {V}", flush=True)
+    # rows of an odd length begin at the same place within 16 bytes every 8 rows, and a row's
+    # sums run in an order that this place decides: repetitions k and k + 8 are the same
+    kl, dz, stats = call(8)  # (400 rows: a block per row)
+    big_kl, big_dz, big_stats = call(times)
+    assert times >= 16
+    for k in range(0, times - 7, 8):
+        assert torch.equal(big_kl[k:k + 8], kl) and torch.equal(big_dz[k:k + 8], dz)
+    assert big_stats[0].item() == times * stats[0].item() / 8
 
 
 def test_forward_alone_gives_the_same_divergence():

@@ -42,7 +42,8 @@ def _cuda(a):
 
 @pytest.mark.parametrize("T,d,V,scale,masked", [
     (1, 8, 1, 1.0, False), (1, 64, 1024, 8.0, False), (7, 896, 500, 0.5, True),
-    (513, 72, 4097, 1.7, True), (300, 3584, 77, 1.0, False), (4099, 8, 11, 59.866, True)])
+    (513, 72, 4097, 1.7, True), (300, 3584, 77, 1.0, False), (4099, 8, 11, 59.866, True),
+    (1203, 3584, 300, 0.7, True)])
 def test_lookup(T, d, V, scale, masked):
     rbp = require_gpu()
     rng = np.random.default_rng(T + d)
@@ -155,3 +156,32 @@ def test_gradient_by_differences():
     rbp.policy_embed_bwd(r, y, None, dW, rbp.workspace(rbp.RBP_OP_EMBED_BWD, T, d, V), scale=scale)
     difference = ((out[0].double() - out[1].double()) * r.double()).sum().item() / 2
     assert difference == (dW.double() * step.double()).sum().item()  # small integers: exact
+
+
+@pytest.mark.parametrize("T,d,V,kind", [(7001, 448, 150001, "skewed"), (12289, 448, 150001, "runs"),
+                                        (6145, 8, 511, "runs"), (20001, 24, 512, "skewed"),
+                                        (600001, 8, 900, "runs")])
+def test_gradient_written_whole_on_every_route(T, d, V, kind):
+    """One block beside the clearing of dW; tiles with one, two and three digits; the longest
+    slices."""
+    _check_backward(require_gpu(), T, d, V, kind, torch.float32, False)
+
+
+def test_gradient_of_a_table_with_four_digits():
+    rbp = require_gpu()
+    V, d, T = (1 << 27) + 3, 8, 9001
+    rng = np.random.default_rng(8)
+    ids = np.unique(np.concatenate([rng.integers(0, V, 300), [0, V - 1, 1 << 26, (1 << 27) - 1]]))
+    y = ids[rng.integers(0, len(ids), T)].astype(np.int32)
+    dx = rng.standard_normal((T, d)).astype(np.float32)
+    dW = torch.zeros((V, d), device="cuda")
+    rbp.policy_embed_bwd(_cuda(dx), _cuda(y), None, dW,
+                         rbp.workspace(rbp.RBP_OP_EMBED_BWD, T, d, V), accumulate_dW=True)
+    place = np.searchsorted(ids, y)
+    want = vocab.embed_backward(dx, place, None, len(ids))
+    size = vocab.embed_backward(np.abs(dx), place, None, len(ids))
+    count = np.bincount(place, minlength=len(ids))[:, None]
+    rows = torch.from_numpy(ids).cuda()
+    assert np.all(np.abs(to_np(dW[rows]) - want) <= (count + 2) * F32 * size)
+    dW[rows] = 0.0
+    assert not dW.any()

@@ -79,7 +79,8 @@ def _case(B, K, V, dtype, drafted, seed, sd=2.0):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("drafted", [True, False])
 @pytest.mark.parametrize("B,K,V", [(1, 1, 1), (3, 2, 2), (5, 1, 63), (4, 3, 65), (2, 7, 1000),
-                                   (9, 4, 1025), (3, 2, 8191), (2, 1, 20001), (2, 2, 151937)])
+                                   (9, 4, 1025), (3, 2, 8191), (2, 1, 20001), (2, 2, 151937),
+                                   (30, 1, 70001), (24, 1, 200003), (2, 255, 50)])
 def test_verified_tokens(B, K, V, drafted, dtype):
     rbp = require_gpu()
     z, zd, x, u, rng = _case(B, K, V, dtype, drafted, B + K + V)
@@ -89,7 +90,8 @@ def test_verified_tokens(B, K, V, drafted, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("B,V", [(1, 1), (1, 7), (200, 300), (3, 4096), (5, 70001)])
+@pytest.mark.parametrize("B,V", [(1, 1), (1, 7), (200, 300), (3, 4096), (5, 70001), (1, 400001),
+                                 (70, 70001)])
 def test_sampling_without_drafts(B, V, dtype):
     rbp = require_gpu()
     z, _, _, u, _ = _case(B, 0, V, dtype, True, V)
@@ -197,3 +199,29 @@ def test_repeated_calls_and_workspace_contents():
         got.append(out)
     for out in got[1:]:
         assert all(torch.equal(p, q) for p, q in zip(got[0], out))
+
+
+@pytest.mark.parametrize("drafted", [True, False])
+def test_logits_far_from_zero(drafted):
+    """Around 1e8 an fp32 step is 8, and the exponent of the largest logit would not fit the table's
+    arithmetic."""
+    rbp = require_gpu()
+    rng = np.random.default_rng(41)
+    B, K, V = 12, 2, 3000
+    z = 1e8 + 8.0 * rng.integers(-3, 1, (B, K + 1, V))
+    z[B // 2:] *= -1.0
+    zd = z[:, :K] + 8.0 * rng.integers(-1, 2, (B, K, V))
+    x = rng.integers(0, V, (B, K)).astype(np.int32)
+    u = (rng.random((B, K + 1)) * 1.2 - 0.2).clip(0).astype(np.float32)
+    _run(rbp, z, zd if drafted else None, x, None, u)
+    _run(rbp, z, zd if drafted else None, x, None, u, 16.0, pad=1)
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -100, 1e-3, 300.0, 1e30])
+def test_extreme_temperatures(tau):
+    rbp = require_gpu()
+    tau = float(np.float32(tau))
+    for drafted in (True, False):
+        z, zd, x, u, _ = _case(7, 2, 1000, torch.float32, drafted, 51)
+        z[0, :, 7:] = -np.inf
+        _run(rbp, z, zd, x, None, u, tau)

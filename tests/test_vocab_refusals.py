@@ -44,14 +44,15 @@ REFUSED = [
                                         dict(out=ctypes.c_void_p(4098)), dict(T=1 << 31)]),
     (_embed_bwd, rbp.RBP_EINVAL, [dict(dx=NULL), dict(tokens=NULL), dict(dW=NULL), dict(T=-1),
                                   dict(d=0), dict(V=0), dict(typ=2), dict(typ=-1),
-                                  dict(scale=math.nan), dict(dW=NULL, T=0)]),
+                                  dict(scale=math.nan), dict(dW=NULL, T=0), dict(ws=ctypes.c_void_p(4104))]),
     (_embed_bwd, rbp.RBP_EUNSUPPORTED, [dict(d=20), dict(dx=ctypes.c_void_p(4100)),
                                         dict(dW=ctypes.c_void_p(4104)), dict(T=(1 << 30) + 1)]),
     (_embed_bwd, rbp.RBP_EWORKSPACE, [dict(ws=NULL), dict(ws_bytes=0), dict(ws_bytes=64)]),
     (_verify, rbp.RBP_EINVAL, [dict(z=NULL), dict(x=NULL), dict(u=NULL), dict(tok=NULL),
                                dict(lp=NULL), dict(n_out=NULL), dict(B=-1), dict(K=-1), dict(V=0),
                                dict(ld=9), dict(ldd=9), dict(typ=7), dict(tau=0.0), dict(tau=-1.0),
-                               dict(tau=math.inf), dict(tau=math.nan), dict(z=ODD), dict(zd=ODD),
+                               dict(tau=math.inf), dict(tau=math.nan), dict(tau=1e-38), dict(tau=1e38),
+                               dict(z=ODD), dict(zd=ODD), dict(ws=ODD),
                                dict(typ=rbp.RBP_F32, z=ctypes.c_void_p(4098))]),
     (_verify, rbp.RBP_EUNSUPPORTED, [dict(K=256), dict(B=1 << 23)]),
     (_verify, rbp.RBP_EWORKSPACE, [dict(ws=NULL), dict(ws_bytes=0)]),
@@ -59,7 +60,8 @@ REFUSED = [
                                 dict(length=NULL), dict(kl=NULL), dict(loss=NULL),
                                 dict(stats=NULL), dict(T=-1), dict(V=0), dict(K=0), dict(B=0),
                                 dict(n_seq=0), dict(ld=9), dict(typ=2), dict(tau=0.0),
-                                dict(tau=math.nan), dict(scale=math.inf), dict(z=ODD),
+                                dict(tau=math.nan), dict(tau=1e-38), dict(tau=1e38), dict(scale=math.inf),
+                                dict(z=ODD), dict(ws=ctypes.c_void_p(4100)),
                                 dict(dz=ctypes.c_void_p(4098))]),
     (_distill, rbp.RBP_EUNSUPPORTED, [dict(K=257), dict(T=1 << 31)]),
     (_distill, rbp.RBP_EWORKSPACE, [dict(ws=NULL), dict(ws_bytes=7)]),
