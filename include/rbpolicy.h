@@ -596,9 +596,12 @@ int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
  * out_logp device fp32 [B, K + 1]: log p of each emitted token (the behaviour
  *         log-prob for rb_push), then 0;
  * n_out   device int32 [B]: tokens emitted, a + 1.
- * Sums, comparisons and the search for the drawn token are carried out in 64 bits,
+ * Comparisons, the search for the drawn token and the sums that decide are in 64 bits,
  * so a decision differs from the exact one only where a border lies within about
- * 1e-12 of u.  Logits of -infinity have probability 0.  A row of logits with a NaN,
+ * 1e-12 of u (2^-25, half a step of u, where a token is drawn from max(p_a - q_a, 0)).
+ * out_logp beside draft_logits comes from 32-bit sums for accepted drafts (off by at
+ * most 5e-6 at V = 2^18), from 64-bit ones else.  Weights max(p_a - q_a, 0) whose total
+ * is below 2^-44 count as all 0.  Logits of -infinity have probability 0.  A row of logits with a NaN,
  * with +infinity, or with -infinity only has no distribution: a draft at such a
  * position of the policy's is rejected, and drawing there emits token -1 with a
  * NaN log-prob; such a row of draft_logits has its draft rejected, and the token
@@ -606,8 +609,8 @@ int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
  * ws      device, >= rbp_workspace_bytes(RBP_OP_VERIFY, B, K, V).
  * Errors: RBP_EINVAL (null pointers, B < 0, K < 0, V < 1, ld or ld_draft < V, an
  *         unknown type, temperature outside [2^-100, 2^100], logits not aligned to
- *         their type or ws to 16 bytes); RBP_EUNSUPPORTED (K above 255, B (K + 1)
- *         above 2^24); RBP_EWORKSPACE.
+ *         their type or ws to 16 bytes); RBP_EUNSUPPORTED (K above 255, B above 2^21
+ *         or B (K + 1) above 2^24); RBP_EWORKSPACE.
  */
 int policy_verify_drafts(const void* logits, const void* draft_logits, int logits_type,
                          int64_t ld, int64_t ld_draft, const int32_t* draft_tokens,

@@ -10,16 +10,18 @@
 //
 // A running sum over 152064 tokens has steps of 1e-5 and less, and its rounding
 // decides which token a u beside a step draws: 32-bit sums would differ from the
-// exact ones in about one draw in a hundred.  So exponentials and sums are in 64
-// bits, whose operations this chip runs at the rate of 32-bit ones (52 lanes a clock
-// and compute unit measured): about 17 per logit, near what its load from HBM
-// leaves time for.
+// exact ones in about one draw in a hundred.  So the sums of the row that is drawn
+// from are in 64 bits, whose operations this chip runs at the rate of 32-bit ones (52
+// lanes a clock and compute unit measured), but an exponential takes 13 of them.
 //
-// Up to three launches.  Every row is cut into segments of consecutive tokens, a
-// wave each (stats): the running sum of a whole row exists only by segments.
-// With a draft's logits, the weights max(p - q, 0) of the rejected position are
-// summed over the same segments (rest).  One block per sequence (finish) finds the
-// segment that u_K falls into, and the token inside it.
+// Every row is cut into segments of consecutive tokens, a wave each: the running sum
+// of a whole row exists only by segments.  Without draft logits, two launches: the
+// segments' 64-bit sums (stats); then a block per sequence (finish) decides, finds the
+// segment that u_K falls into, and the token inside it.  With draft logits, where there
+// are twice the rows and two of them are drawn from, three: 32-bit sums of all rows
+// (rough), which the load of the logits bounds -- 576 rows of 152064 bf16 in 60 us in 64
+// bits --; 64-bit sums of the rows to draw from (exact), whose blocks decide first, an
+// acceptance too near for the rough sums by a 64-bit pass over its two rows; finish.
 
 #include <cmath>
 
@@ -141,6 +143,15 @@ struct Part {
   float m, pad;
 };
 
+// Sums over some tokens of a row to draw from: 2^((z - m) k2) of the policy (p) and of
+// the draft (q), and both over the tokens where the policy's probability is larger (a,
+// b): there max(p - q, 0) = p - q, so its sum is a / sum p - b / sum q.  Which tokens
+// these are is told by the rough sums; `near` is the sum of p over those that they may
+// mistake.
+struct Drawn {
+  double p, q, a, b, near;
+};
+
 struct Args {
   int64_t ld, ld_draft;
   const int32_t *draft_tokens, *n_draft;
@@ -152,8 +163,8 @@ struct Args {
   int32_t* out_tokens;
   float* out_logp;
   int32_t* n_out;
-  Part* parts;   // [B][K + 1 + K][segments]: the policy's rows, then the draft's
-  double* rest;  // [B][segments][kShares]
+  Part* parts;  // [B][K + 1 + K][segments]: the policy's rows, then the draft's
+  Drawn* drawn;  // [B][segments][kShares]
   __device__ __forceinline__ int32_t drafts(int64_t b) const {
     return n_draft == nullptr ? K : min(n_draft[b], K);
   }
@@ -171,35 +182,123 @@ struct Segment {
   }
 };
 
+// The row and segment of a wave of the first launch, none where its position has no
+// draft.
+template <class X>
+struct Place {
+  const X* row;
+  uint32_t row_id;
+  int seg;
+};
+template <bool kDrafts, class X>
+__device__ __forceinline__ Place<X> place_of(const X* logits, const X* draft_logits, const Args& a,
+                                             int64_t n_items) {
+  Place<X> p{nullptr, 0, 0};
+  // (rows times segments may pass 31 bits, rows may not)
+  const int64_t item = (int64_t)blockIdx.x * (blockDim.x >> 6) +
+                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (item >= n_items) return p;
+  p.seg = (int)(item & (a.segments - 1));
+  p.row_id = (uint32_t)(item >> a.log_segments);
+  const uint32_t rows = kDrafts ? 2 * a.K + 1 : a.K + 1;
+  const int64_t b = p.row_id / rows;
+  const int k = (int)(p.row_id % rows);
+  const int32_t n = a.drafts(b);  // (negative: no row)
+  if (k <= a.K) {
+    if (k <= n) p.row = logits + (b * (a.K + 1) + k) * a.ld;
+  } else if constexpr (kDrafts) {
+    const int at = k - a.K - 1;
+    if (at < n) p.row = draft_logits + (b * a.K + at) * a.ld_draft;
+  }
+  return p;
+}
+
 constexpr int kStatsThreads = 256;
 // the reference follows the largest logit once it is that many powers of two above
 constexpr double kSlack = 200.0;
+constexpr float kRoughSlack = 8.0f;
 
-// A wave per segment of a row.
+// A wave per segment of a row, in 32 bits: s by pieces of exponentials whose argument y
+// is off by 3 2^-24 |y|, and they by one unit in the last place.  Weighted by the
+// probabilities, |y| is at most log2 V + 2 kRoughSlack (the entropy bounds the distance
+// from the largest logit; the reference lags behind it, and moves), so the sum of a row
+// of 2^18 tokens is off by 5e-6 of itself at most, one of 2^31 by 7e-6, and p / q by
+// less than kUnsure.
+constexpr double kUnsure = 0x1p-16;
+struct Rough {
+  float m = -INFINITY;
+  double s = 0.0;
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N], float k2, float slack) {
+    float top = x[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) top = fmaxf(top, x[k]);
+    if (top > m + slack) {
+      s *= (double)rbp::lp::exp2_hw((m - top) * k2);
+      m = top;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float e[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) e[k] = rbp::lp::exp2_hw((x[k] - ref) * k2);
+#pragma unroll
+    for (int w = N / 2; w >= 1; w /= 2)
+#pragma unroll
+      for (int k = 0; k < w; ++k) e[k] += e[k + w];
+    s += (double)e[0];
+  }
+};
 template <class X>
-__global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restrict__ logits,
+__global__ void __launch_bounds__(kStatsThreads) rough_kernel(const X* __restrict__ logits,
                                                               const X* __restrict__ draft_logits,
                                                               Args a, int64_t n_items) {
   constexpr int E = Row<X>::E, kBatch = 4;
-  // (rows times segments may pass 31 bits, rows may not)
-  const int64_t item = (int64_t)blockIdx.x * (kStatsThreads / 64) +
-                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place<X> place = place_of<true, X>(logits, draft_logits, a, n_items);
+  if (place.row == nullptr) return;
+  const int lane = threadIdx.x & 63;
+  const Row<X> r(place.row, a.V);
+  const Segment<X> g(r, place.seg, a.log_segments);
+  const float k2 = (float)a.k2, slack = fminf(kRoughSlack / k2, 1e30f);
+  Rough o;
+  for (int32_t c = g.p0 + lane; c < g.p1; c += kBatch * 64) {
+    uint4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * 64 < g.p1) v[i] = *reinterpret_cast<const uint4*>(place.row + r.at(c + i * 64));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (c + i * 64 < g.p1) {
+        float x[E];
+        unpack(v[i], x);
+        o.add(x, k2, slack);
+      }
+  }
+  const int32_t loose = r.loose(lane);
+  if (loose >= 0 && (loose < r.head ? place.seg == 0 : place.seg == a.segments - 1)) {
+    const float x[1] = {value(place.row[loose])};
+    o.add(x, k2, slack);
+  }
+  float M = o.m;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+  double s = o.s;
+  if (o.m != M) s *= exp2_d(((double)o.m - (double)M) * a.k2);
+  s = wave_sum(s);
+  if (lane == 0) a.parts[(int64_t)place.row_id * a.segments + place.seg] = Part{s, M, 0.0f};
+}
+
+// A wave per segment of a row, in 64 bits.
+template <class X>
+__global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restrict__ logits,
+                                                              Args a, int64_t n_items) {
+  constexpr int E = Row<X>::E, kBatch = 4;
   __shared__ double roots[kRoots];
   if (threadIdx.x < kRoots) roots[threadIdx.x] = g_roots[threadIdx.x];
   __syncthreads();
-  if (item >= n_items) return;
-  const int lane = threadIdx.x & 63;
-  const int seg = (int)(item & (a.segments - 1));
-  const uint32_t rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
-  const uint32_t row_id = (uint32_t)(item >> a.log_segments);
-  const int64_t b = row_id / rows;
-  const int k = (int)(row_id % rows);
-  const int32_t n = a.drafts(b);
-  const bool drafted = k > a.K;
-  const int at = drafted ? k - a.K - 1 : k;
-  if (drafted ? at >= n : at > n) return;  // (n < 0: no row)
-  const X* row = drafted ? draft_logits + (b * a.K + at) * a.ld_draft
-                         : logits + (b * (a.K + 1) + at) * a.ld;
+  const Place<X> place = place_of<false, X>(logits, nullptr, a, n_items);
+  if (place.row == nullptr) return;
+  const X* row = place.row;
+  const int seg = place.seg, lane = threadIdx.x & 63;
   const Row<X> r(row, a.V);
   const Segment<X> g(r, seg, a.log_segments);
   float m = -INFINITY, top = -INFINITY;
@@ -270,7 +369,8 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
                              : ((double)m - (double)M) * a.k2);
   s = wave_sum(s);
   if (lane == 0)
-    a.parts[(int64_t)row_id * a.segments + seg] = Part{top != top ? (double)NAN : s, M, 0.0f};
+    a.parts[(int64_t)place.row_id * a.segments + seg] =
+        Part{top != top ? (double)NAN : s, M, 0.0f};
 }
 
 // A row's reference and sum from its segments, by one wave; sum is NaN or 0 where
@@ -296,7 +396,7 @@ __device__ __forceinline__ Dist dist_of(const Part* parts, int n, double k2, int
 }
 
 constexpr int kMaxK = 255;
-constexpr int kShares = 2;  // waves of a segment in rest_kernel
+constexpr int kShares = 2;  // waves of a segment in exact_kernel
 constexpr int kFinishThreads = 1024;
 constexpr int kRun = 5;  // tokens of a thread: a segment of 152064 / 32 in one tile
 constexpr int kMaxSegments = 64;
@@ -308,58 +408,112 @@ struct Decision {
   Dist p, q;
 };
 
-// By a block, which takes the rows' distributions into LDS: the policy's of the
-// positions 0 .. n, then the draft's.
+// Whether draft k is accepted: 0 yes, 1 no, 2 too near for sums that are off by up to
+// `unsure`.
 template <class X>
+__device__ __forceinline__ int test_draft(const X* __restrict__ logits,
+                                          const X* __restrict__ draft_logits, const Args& a,
+                                          int64_t b, int k, const Dist& p, const Dist* q,
+                                          double unsure) {
+  const int32_t x = a.draft_tokens[b * a.K + k];
+  if (x < 0 || x >= a.V || !p.valid()) return 1;
+  const double px = exp2_d(p.log2_of(value(logits[(b * (a.K + 1) + k) * a.ld + x]), a.k2));
+  double qx = 1.0;
+  if (q != nullptr) {
+    if (!q->valid()) return 1;
+    qx = exp2_d(q->log2_of(value(draft_logits[(b * a.K + k) * a.ld_draft + x]), a.k2));
+  }
+  const double uq = (double)a.u[b * (a.K + 1) + k] * qx;
+  if (px > 0.0 && fabs(uq - px) < unsure * px) return 2;
+  return uq < px ? 0 : 1;
+}
+
+// A row's sum in 64 bits, by a block.
+template <class X>
+__device__ double exact_sum(const X* __restrict__ row, int32_t V, double m, double k2,
+                            double* wave_s) {
+  double s = 0.0;
+#pragma unroll 4
+  for (int32_t v = threadIdx.x; v < V; v += blockDim.x)
+    s += exp2_d(((double)value(row[v]) - m) * k2);
+  s = wave_sum(s);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) wave_s[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += wave_s[w];
+  return s;
+}
+
+// By a block, which takes the rows' distributions into LDS: the policy's of the
+// positions 0 .. n, then the draft's.  kRough: the sums are rough.
+struct DecideLds {
+  int32_t first, code;
+  double wave_s[16];
+};
+template <class X, bool kRough>
 __device__ void decide(const X* __restrict__ logits, const X* __restrict__ draft_logits,
-                       const Args& a, int64_t b, int32_t n, Dist* rows_s, Decision* out) {
+                       const Args& a, int64_t b, int32_t n, Dist* rows_s, DecideLds* lds,
+                       Decision* out) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
+  const int rows = kRough ? 2 * a.K + 1 : a.K + 1;
   const Part* parts = a.parts + b * rows * a.segments;
-  for (int k = wave; k <= 2 * n; k += waves) {  // row k of the policy, or k - n - 1 of the draft
-    if (k > n && draft_logits == nullptr) break;
+  // row k of the policy, or k - n - 1 of the draft
+  for (int k = wave; k <= (kRough ? 2 * n : n); k += waves) {
     const int row = k <= n ? k : a.K + 1 + (k - n - 1);
     const Dist d = dist_of(parts + row * a.segments, a.segments, a.k2, lane);
     if (lane == 0) rows_s[k] = d;
   }
-  __syncthreads();
-  // the first draft that is not accepted, 64 at a time
-  if (wave == 0) {
-    int32_t first = n;
-    for (int k0 = 0; k0 < n && first == n; k0 += 64) {
-      const int k = k0 + lane;
-      bool ok = true;
-      if (k < n) {
-        const int32_t x = a.draft_tokens[b * a.K + k];
-        const Dist p = rows_s[k];
-        ok = x >= 0 && x < a.V && p.valid();
-        if (ok) {
-          const double px =
-              exp2_d(p.log2_of(value(logits[(b * (a.K + 1) + k) * a.ld + x]), a.k2));
-          double qx = 1.0;
-          if (draft_logits != nullptr) {
-            const Dist q = rows_s[n + 1 + k];
-            qx = q.valid()
-                     ? exp2_d(q.log2_of(value(draft_logits[(b * a.K + k) * a.ld_draft + x]), a.k2))
-                     : NAN;
-          }
-          ok = (double)a.u[b * (a.K + 1) + k] * qx < px;
+  // the first draft from `from` on that is not accepted, 64 at a time
+  auto search = [&](int32_t from) {
+    __syncthreads();
+    if (wave == 0) {
+      int32_t first = n;
+      int code = 0;
+      for (int k0 = from; k0 < n && first == n; k0 += 64) {
+        const int k = k0 + lane;
+        const int c = k < n ? test_draft(logits, draft_logits, a, b, k, rows_s[k],
+                                         kRough ? rows_s + n + 1 + k : nullptr,
+                                         kRough ? kUnsure : 0.0)
+                            : 0;
+        const uint64_t no = __ballot(c != 0);
+        if (no != 0) {
+          const int j = __builtin_ctzll(no);
+          first = k0 + j;
+          code = __shfl(c, j, 64);
         }
       }
-      const uint64_t no = __ballot(!ok);
-      if (no != 0) first = k0 + __builtin_ctzll(no);
+      if (lane == 0) {
+        lds->first = first;
+        lds->code = code;
+      }
     }
-    if (lane == 0) {
-      const bool drawn_from_p = first == n;
-      out->accepted = first;
-      out->x = drawn_from_p ? -1 : a.draft_tokens[b * a.K + first];
-      out->p = rows_s[first];
-      out->q = rows_s[drawn_from_p || draft_logits == nullptr ? first : n + 1 + first];
-      out->kind = !out->p.valid() ? -1
-                  : drawn_from_p ? 0
-                  : draft_logits == nullptr ? (out->x >= 0 && out->x < a.V ? 1 : 0)
-                  : out->q.valid() ? 2 : 0;
+    __syncthreads();
+  };
+  search(0);
+  if constexpr (kRough) {
+    while (lds->code == 2) {  // too near: both rows again in 64 bits
+      const int32_t k = lds->first;
+      Dist p = rows_s[k], q = rows_s[n + 1 + k];
+      p.sum = exact_sum(logits + (b * (a.K + 1) + k) * a.ld, a.V, p.m, a.k2, lds->wave_s);
+      q.sum = exact_sum(draft_logits + (b * a.K + k) * a.ld_draft, a.V, q.m, a.k2, lds->wave_s);
+      p.ls = log2(p.sum);
+      q.ls = log2(q.sum);
+      if (test_draft(logits, draft_logits, a, b, k, p, &q, 0.0) != 0) break;
+      search(k + 1);
     }
+  }
+  if (threadIdx.x == 0) {
+    const int32_t first = lds->first;
+    const bool drawn_from_p = first == n;
+    out->accepted = first;
+    out->x = drawn_from_p ? -1 : a.draft_tokens[b * a.K + first];
+    out->p = rows_s[first];
+    out->q = rows_s[drawn_from_p || !kRough ? first : n + 1 + first];
+    out->kind = !out->p.valid() ? -1
+                : drawn_from_p ? 0
+                : !kRough ? (out->x >= 0 && out->x < a.V ? 1 : 0)
+                : out->q.valid() ? 2 : 0;
   }
   __syncthreads();
 }
@@ -410,23 +564,25 @@ __device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logit
   return w;
 }
 
-constexpr int kRestThreads = 512;
+constexpr int kExactThreads = 512;
 
-// Sums of max(p - q, 0) over the segments of the rejected position, a wave each.
+// With draft logits: the decision, and the sums of the rows to draw from, a wave per
+// share of a segment.
 template <class X>
-__global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict__ logits,
-                                                            const X* __restrict__ draft_logits,
-                                                            Args a, Decision* decisions) {
+__global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restrict__ logits,
+                                                              const X* __restrict__ draft_logits,
+                                                              Args a, Decision* decisions) {
   __shared__ Dist rows_s[2 * kMaxK + 1];
   __shared__ Decision d_s;
+  __shared__ DecideLds lds;
   __shared__ double roots[kRoots];
-  constexpr int kWaves = kRestThreads / 64;
+  constexpr int kWaves = kExactThreads / 64;
   if (threadIdx.x < kRoots) roots[threadIdx.x] = g_roots[threadIdx.x];
   const unsigned blocks = (a.segments * kShares + kWaves - 1) / kWaves;
   const int64_t b = blockIdx.x / blocks;
   const int32_t n = a.drafts(b);
   if (n < 0) return;
-  decide(logits, draft_logits, a, b, n, rows_s, &d_s);
+  decide<X, true>(logits, draft_logits, a, b, n, rows_s, &lds, &d_s);
   const int part = blockIdx.x % blocks;
   if (part == 0) {
     if (threadIdx.x == 0) decisions[b] = d_s;
@@ -434,37 +590,51 @@ __global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict_
   }
   const int item = part * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int seg = item / kShares, share = item % kShares;
-  if (d_s.kind != 2 || seg >= a.segments) return;
-  const Weight<X> w = weight_of(d_s, logits, draft_logits, a, b);
-  const Row<X> r(w.p, a.V);
+  if (d_s.kind < 0 || seg >= a.segments) return;
+  const bool two = d_s.kind == 2;
+  const X* rp = logits + (b * (a.K + 1) + d_s.accepted) * a.ld;
+  const X* rq = two ? draft_logits + (b * a.K + d_s.accepted) * a.ld_draft : rp;
+  const Row<X> r(rp, a.V);
   const Segment<X> g(r, seg, a.log_segments);
   // the pieces are the policy's row's; the draft's elements may lie otherwise
-  const bool vec =
-      ((reinterpret_cast<uintptr_t>(w.p) ^ reinterpret_cast<uintptr_t>(w.q)) & 15) == 0;
+  const bool vec = ((reinterpret_cast<uintptr_t>(rp) ^ reinterpret_cast<uintptr_t>(rq)) & 15) == 0;
   constexpr int E = Row<X>::E, kBatch = 2;
-  // p = 2^(z k2 - shift) cp, and q likewise: max(p - q, 0) = cp max(.. - .. cq / cp, 0)
+  // a grid's exponentials times 2^(shift - m k2) are relative to the row's largest logit
   Grid gp, gq;
-  gp.refer(w.mp, a.k2, a.span);
-  gq.refer(w.mq, a.k2, a.span);
+  const double mq = two ? d_s.q.m : d_s.p.m;
+  gp.refer(d_s.p.m, a.k2, a.span);
+  gq.refer(mq, a.k2, a.span);
   const bool near = gp.near && gq.near;
-  const double cp = near ? exp2_d(fma(-w.mp, a.k2, gp.shift) - w.lp) : 1.0;
-  const double ratio = near ? exp2_d(fma(-w.mq, a.k2, gq.shift) - w.lq) / cp : 1.0;
-  double s = 0.0;
-  const int32_t p0 = g.p0 + (g.p1 - g.p0) * share / kShares,
-                p1 = g.p0 + (g.p1 - g.p0) * (share + 1) / kShares;
+  const double fp = near ? exp2_d(fma(-d_s.p.m, a.k2, gp.shift)) : 1.0;
+  const double fq = near ? exp2_d(fma(-mq, a.k2, gq.shift)) : 1.0;
+  // p > q by the rough sums
+  const double odds = fq * d_s.p.sum / (fp * d_s.q.sum);
+  Drawn s{0.0, 0.0, 0.0, 0.0, 0.0};
+  auto add = [&](double p, double q, double o) {
+    const double d = fma(-q, o, p);
+    const bool larger = d > 0.0;
+    s.p += p;
+    s.q += q;
+    s.a += larger ? p : 0.0;
+    s.b += larger ? q : 0.0;
+    if (fabs(d) < kUnsure * p) s.near += p;
+  };
+  const int32_t p0 = g.p0 + (int32_t)((int64_t)(g.p1 - g.p0) * share / kShares),
+                p1 = g.p0 + (int32_t)((int64_t)(g.p1 - g.p0) * (share + 1) / kShares);
   for (int32_t c = p0 + lane; c < p1; c += kBatch * 64) {
     uint4 zp[kBatch], zq[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (c + i * 64 >= p1) continue;
       const int32_t at = r.at(c + i * 64);
-      zp[i] = *reinterpret_cast<const uint4*>(w.p + at);
+      zp[i] = *reinterpret_cast<const uint4*>(rp + at);
+      if (!two) continue;
       if (vec) {
-        zq[i] = *reinterpret_cast<const uint4*>(w.q + at);
+        zq[i] = *reinterpret_cast<const uint4*>(rq + at);
       } else {
         X e[E];
 #pragma unroll
-        for (int k = 0; k < E; ++k) e[k] = w.q[at + k];
+        for (int k = 0; k < E; ++k) e[k] = rq[at + k];
         __builtin_memcpy(&zq[i], e, 16);
       }
     }
@@ -473,18 +643,29 @@ __global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict_
       if (c + i * 64 < p1) {
         float p[E], q[E];
         unpack(zp[0], p);
-        unpack(zq[0], q);
+        if (two) unpack(zq[0], q);
         if (near) {
-          Scaled e[E], f[E];
-          gp(p, roots, e);
-          gq(q, roots, f);
+          // four at a time: eight take registers that a second block needs
 #pragma unroll
-          for (int k = 0; k < E; ++k)
-            s += fmax(fma(e[k].p, e[k].root, -(f[k].p * ratio) * f[k].root), 0.0);
+          for (int h = 0; h < E; h += 4) {
+            const float p4[4] = {p[h], p[h + 1], p[h + 2], p[h + 3]};
+            Scaled e[4], f[4];
+            gp(p4, roots, e);
+            if (two) {
+              const float q4[4] = {q[h], q[h + 1], q[h + 2], q[h + 3]};
+              gq(q4, roots, f);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) add(e[k].p * e[k].root, f[k].p * f[k].root, odds);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) s.p = fma(e[k].p, e[k].root, s.p);
+            }
+          }
         } else {
 #pragma unroll 1
           for (int k = 0; k < E; ++k) {
-            s += w.rest(p[0], q[0]);
+            add(exp2_d(((double)p[0] - d_s.p.m) * a.k2),
+                two ? exp2_d(((double)q[0] - d_s.q.m) * a.k2) : 0.0, odds);
 #pragma unroll
             for (int j = 1; j < E; ++j) p[j - 1] = p[j], q[j - 1] = q[j];
           }
@@ -494,11 +675,20 @@ __global__ void __launch_bounds__(kRestThreads) rest_kernel(const X* __restrict_
       for (int k = 1; k < kBatch; ++k) zp[k - 1] = zp[k], zq[k - 1] = zq[k];
     }
   }
+  s.p *= fp, s.a *= fp, s.near *= fp, s.q *= fq, s.b *= fq;
   const int32_t loose = r.loose(lane);
   if (share == 0 && loose >= 0 && (loose < r.head ? seg == 0 : seg == a.segments - 1))
-    s += w.rest(value(w.p[loose]), value(w.q[loose])) / cp;
-  s = wave_sum(s) * cp;
-  if (lane == 0) a.rest[b * a.segments * kShares + item] = s;
+    add(exp2_d(((double)value(rp[loose]) - d_s.p.m) * a.k2),
+        two ? exp2_d(((double)value(rq[loose]) - d_s.q.m) * a.k2) : 0.0,
+        d_s.p.sum / d_s.q.sum);
+  s.p = wave_sum(s.p);
+  if (two) {
+    s.q = wave_sum(s.q);
+    s.a = wave_sum(s.a);
+    s.b = wave_sum(s.b);
+    s.near = wave_sum(s.near);
+  }
+  if (lane == 0) a.drawn[b * a.segments * kShares + item] = s;
 }
 
 // A block per sequence.
@@ -510,18 +700,21 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
   constexpr int kWaves = kFinishThreads / 64;
   __shared__ Dist rows_s[kMaxK + 1];
   __shared__ Decision d_s;
+  __shared__ DecideLds lds;
   __shared__ double seg_s[kMaxSegments], wave_s[kWaves], wt_s[kRun][kFinishThreads];
   __shared__ int32_t found, last;
+  __shared__ uint64_t fixes_s;
   const int64_t b = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t n = a.drafts(b);
   const double u = (double)a.u[b * (a.K + 1) + a.K];
-  // (what the rest's launch left, should there be one: loaded with the decision)
-  double rest = 0.0;
+  // (what the exact sums' launch left, should there be one: loaded with the decision)
+  Drawn drawn{0.0, 0.0, 0.0, 0.0, 0.0};
   if (draft_logits != nullptr && tid < a.segments) {
     static_assert(kShares == 2, "two sums");
-    const double* q = a.rest + (b * a.segments + tid) * kShares;
-    rest = q[0] + q[1];
+    const Drawn* d = a.drawn + (b * a.segments + tid) * kShares;
+    drawn = Drawn{d[0].p + d[1].p, d[0].q + d[1].q, d[0].a + d[1].a, d[0].b + d[1].b,
+                  d[0].near + d[1].near};
   }
   if (n < 0) {
     for (int k = tid; k <= a.K; k += kFinishThreads) {
@@ -533,10 +726,32 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
   }
   const int rows = draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1;
   if (draft_logits == nullptr) {
-    decide(logits, draft_logits, a, b, n, rows_s, &d_s);
+    decide<X, false>(logits, nullptr, a, b, n, rows_s, &lds, &d_s);
     emit_accepted(logits, a, b, d_s, rows_s);
   } else {
     if (tid == 0) d_s = decisions[b];
+    __syncthreads();
+    if (d_s.kind < 0) return;
+    // The exact sums of both rows, and the segments' of max(p - q, 0).  The rough odds
+    // were off by `off`, so a segment's is by off times what lay near them at most: where
+    // that is more than 2^-30 of the total (u has steps of 2^-24) it is summed again.
+    static_assert(kMaxSegments <= 64, "a lane per segment");
+    if (wave == 0) {
+      const double p = wave_sum(drawn.p), q = wave_sum(drawn.q);
+      const double off = fabs(d_s.p.sum * q / (d_s.q.sum * p) - 1.0);
+      const double rest = drawn.a / p - drawn.b / q;
+      const double mine = rest > 0x1p-900 ? rest : 0.0;  // (2^-1000 a token may be nothing)
+      const double total = wave_sum(mine);
+      if (lane < a.segments) seg_s[lane] = mine;
+      const uint64_t fixes = __ballot(off * drawn.near > 0x1p-30 * total * p);
+      if (lane == 0) {
+        fixes_s = fixes;
+        d_s.p.sum = p;
+        d_s.p.ls = log2(p);
+        d_s.q.sum = q;
+        d_s.q.ls = log2(q);
+      }
+    }
     __syncthreads();
   }
   if (d_s.kind < 0) return;
@@ -547,32 +762,30 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
 
   Weight<X> w = weight_of(d_s, logits, draft_logits, a, b);
   auto segments_of_p = [&] {
-    if (tid < a.segments) {
+    if (tid >= a.segments) return;
+    if (draft_logits != nullptr) {
+      seg_s[tid] = drawn.p;
+    } else {
       const Part p = parts[tid];
       seg_s[tid] = p.m == d_s.p.m ? p.s : p.s * exp2_d(((double)p.m - d_s.p.m) * a.k2);
     }
   };
-  if (w.kind == 2) {
-    // (2^-1000 a token, where they have nothing left)
-    if (tid < a.segments) seg_s[tid] = rest > 0x1p-900 ? rest : 0.0;
-  } else {
-    segments_of_p();
-  }
+  if (w.kind != 2) segments_of_p();
   if (tid == 0) {
     found = a.V;
     last = -1;
   }
-  // First, where the draft has to be left out, the sum of its segment without it;
-  // then the segment that the token falls into: the first whose end lies behind the
+  // First the segments to sum again (`fixes`), for the draft that has to be left out
+  // among them; then the segment that the token falls into: the first whose end lies behind the
   // goal, after it the next ones, should rounding leave the token to them, or the
   // last with any weight where none does (u at the end of its interval).  One loop
   // over segments for both, and one copy of the exponential, for the sake of code
   // that has to be fetched.
-  int fix = -1;
+  uint64_t fixes = w.kind == 2 ? fixes_s : 0;
   if (w.kind == 1) {
     const int32_t piece = w.x < r.head ? 0 : (w.x - r.head) / Row<X>::E;
-    fix = r.pieces > 0 ? min((int)(((int64_t)piece << a.log_segments) / r.pieces), a.segments - 1)
-                       : a.segments - 1;
+    int fix = r.pieces > 0 ? min((int)(((int64_t)piece << a.log_segments) / r.pieces), a.segments - 1)
+                           : a.segments - 1;
     while (fix < a.segments - 1 && w.x >= Segment<X>(r, fix, a.log_segments).v1) ++fix;
     while (fix > 0 && w.x < Segment<X>(r, fix, a.log_segments).v0) --fix;
     // Taken off its segment's sum where that is exact enough: the two exponentials
@@ -585,15 +798,16 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
     __syncthreads();
     if (left >= 0x1p-20 * e && rest >= 0.125 * e) {
       if (tid == 0) seg_s[fix] = left;
-      fix = -1;
+    } else {
+      fixes = 1ull << fix;
     }
   }
-  uint64_t todo = 0;
+  uint64_t todo = 0, some = 0;
   double scan = 0.0, goal = 0.0;
   bool located = false;
   for (;;) {
     __syncthreads();
-    if (fix < 0 && !located) {
+    if (fixes == 0 && !located) {
       for (;;) {
         const double mine = lane < a.segments ? seg_s[lane] : 0.0;
         scan = mine;
@@ -603,9 +817,10 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
           if (lane >= off) scan += o;
         }
         const double total = __shfl(scan, 63, 64);
-        if (total > 0.0 || w.kind == 0) {
+        // (max(p - q, 0) below 2^-44 is the sums' rounding)
+        if (total > (w.kind == 2 ? 0x1p-44 : 0.0) || w.kind == 0) {
           goal = u * total;
-          const uint64_t some = __ballot(mine > 0.0);
+          some = __ballot(mine > 0.0);
           todo = __ballot(mine > 0.0 && scan > goal);
           if (todo == 0 && some != 0) todo = 1ull << (63 - __builtin_clzll(some));
           break;
@@ -619,8 +834,11 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
       }
       located = true;
     }
-    if (fix < 0 && todo == 0) break;
-    const int seg = fix >= 0 ? fix : __builtin_ctzll(todo);
+    // (a segment may turn out to hold no weight after all: then the one before)
+    if (fixes == 0 && todo == 0 && last < 0 && some != 0)
+      todo = 1ull << (63 - __builtin_clzll(some));
+    if (fixes == 0 && todo == 0) break;
+    const int seg = __builtin_ctzll(fixes != 0 ? fixes : todo);
     const Segment<X> g(r, seg, a.log_segments);
     double before = __shfl(scan, seg > 0 ? seg - 1 : 0, 64);
     if (seg == 0) before = 0.0;
@@ -669,7 +887,7 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
         if (q < wave) run += wave_s[q];
         sum += wave_s[q];
       }
-      if (fix >= 0) continue;
+      if (fixes != 0) continue;
       run += upto - s;
       int32_t hit = a.V, end = -1;
 #pragma unroll
@@ -691,11 +909,12 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
       done = found < a.V;
     }
     if (done) break;
-    if (fix >= 0) {
-      if (tid == 0) seg_s[fix] = sum;
-      fix = -1;
+    if (fixes != 0) {
+      if (tid == 0) seg_s[seg] = sum;
+      fixes &= fixes - 1;
     } else {
       todo &= todo - 1;
+      some &= ~(1ull << seg);
     }
   }
   if (tid == 0) {
@@ -708,17 +927,19 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
 
 // Segments of a row: 512 tokens or more each, and up to 64, a lane each to join them
 // (32 with many rows: 576 rows of 152064 bf16 take 75 us in 64 segments, 68 in 32;
-// 5 rows 5.6 and 8.3).
+// 5 rows 5.6 and 8.3); fewer where rows alone fill the chip many times over, since a
+// launch has less than 2^32 threads.
 int segments_of(int64_t B, int64_t K, int32_t V) {
-  const int most = B * (2 * K + 1) <= 64 ? kMaxSegments : kMaxSegments / 2;
+  const int64_t rows = B * (2 * K + 1);
+  const int most = rows <= 64 ? kMaxSegments : kMaxSegments / 2;
   int n = 1;
-  while (n < most && V / (2 * n) >= 512) n *= 2;
+  while (n < most && V / (2 * n) >= 512 && rows * n < (1 << 20)) n *= 2;
   return n;
 }
 
 struct VerifyWs {
   Part* parts;
-  double* rest;
+  Drawn* drawn;
   Decision* decisions;
   size_t bytes;
 };
@@ -727,7 +948,7 @@ VerifyWs carve_verify(void* base, int64_t B, int64_t K, int32_t V) {
   VerifyWs w;
   const size_t segments = (size_t)segments_of(B, K, V);
   w.parts = c.take<Part>((size_t)B * (2 * K + 1) * segments);
-  w.rest = c.take<double>((size_t)B * segments * kShares);
+  w.drawn = c.take<Drawn>((size_t)B * segments * kShares);
   w.decisions = c.take<Decision>((size_t)B);
   w.bytes = rbp::align_up(c.used, 256);
   return w;
@@ -738,12 +959,17 @@ void launch(const X* logits, const X* draft_logits, const Args& a, Decision* dec
             hipStream_t s) {
   const int64_t rows = a.B * (int64_t)(draft_logits == nullptr ? a.K + 1 : 2 * a.K + 1);
   const int64_t items = rows * a.segments;
-  hipLaunchKernelGGL(stats_kernel<X>, dim3((unsigned)rbp::ceil_div(items, kStatsThreads / 64)),
-                     dim3(kStatsThreads), 0, s, logits, draft_logits, a, items);
-  if (draft_logits != nullptr)
-    hipLaunchKernelGGL(rest_kernel<X>,
-                       dim3((unsigned)(a.B * rbp::ceil_div(a.segments * kShares, kRestThreads / 64))),
-                       dim3(kRestThreads), 0, s, logits, draft_logits, a, decisions);
+  const dim3 grid((unsigned)rbp::ceil_div(items, kStatsThreads / 64));
+  if (draft_logits == nullptr) {
+    hipLaunchKernelGGL(stats_kernel<X>, grid, dim3(kStatsThreads), 0, s, logits, a, items);
+  } else {
+    hipLaunchKernelGGL(rough_kernel<X>, grid, dim3(kStatsThreads), 0, s, logits, draft_logits, a,
+                       items);
+    hipLaunchKernelGGL(exact_kernel<X>,
+                       dim3((unsigned)(a.B * rbp::ceil_div(a.segments * kShares,
+                                                           kExactThreads / 64))),
+                       dim3(kExactThreads), 0, s, logits, draft_logits, a, decisions);
+  }
   hipLaunchKernelGGL(finish_kernel<X>, dim3(a.B), dim3(kFinishThreads), 0, s, logits, draft_logits,
                      a, decisions);
 }
@@ -767,8 +993,8 @@ extern "C" int policy_verify_drafts(const void* logits, const void* draft_logits
               "policy_verify_drafts: unknown logits_type %d", logits_type);
   RBP_REQUIRE(temperature >= 0x1p-100f && temperature <= 0x1p100f, RBP_EINVAL,
               "policy_verify_drafts: temperature must lie in [2^-100, 2^100]");
-  RBP_REQUIRE(K <= 255 && (int64_t)B * (K + 1) <= (1 << 24), RBP_EUNSUPPORTED,
-              "policy_verify_drafts: K above 255 or B (K + 1) above 2^24");
+  RBP_REQUIRE(K <= 255 && B <= (1 << 21) && (int64_t)B * (K + 1) <= (1 << 24), RBP_EUNSUPPORTED,
+              "policy_verify_drafts: K above 255, B above 2^21 or B (K + 1) above 2^24");
   if (B == 0) return RBP_OK;
   RBP_REQUIRE(logits && u && out_tokens && out_logp && n_out && (K == 0 || draft_tokens),
               RBP_EINVAL, "policy_verify_drafts: null pointer");
@@ -785,7 +1011,7 @@ extern "C" int policy_verify_drafts(const void* logits, const void* draft_logits
   const double k2 = kLog2eD / (double)temperature;
   const Args a{ld,  ld_draft, draft_tokens, n_draft, u, B, K, V, segments,
                __builtin_ctz((unsigned)segments), k2, 1000.0 / k2,
-               (float)std::fmin(kSlack / k2, 1e30), out_tokens, out_logp, n_out, w.parts, w.rest};
+               (float)std::fmin(kSlack / k2, 1e30), out_tokens, out_logp, n_out, w.parts, w.drawn};
   if (logits_type == RBP_F32)
     launch(static_cast<const float*>(logits), static_cast<const float*>(draft_logits), a,
            w.decisions, s);

@@ -1,6 +1,11 @@
 """policy_verify_drafts against oracle/vocab.py: tokens and counts equal, log-probs to their
 rounding (fp32: half a step, 2^-24 of the value; the 64-bit sums before it are off by less than
-1e-9)."""
+1e-9).  Beside draft logits the log-probs of accepted drafts come from 32-bit exponentials: one
+of argument y (in powers of two) is off by 3 2^-24 ln 2 |y| for the roundings of the difference,
+the factor and the product, and by 2^-23 for its own; weighted by the probabilities |y| is at most
+log2 V, plus the 8 that the reference may lag and the 8 by which it then moves, 18 + 16 here, so
+the log of the sum is off by 34 * 3 * 2^-24 * 0.7 + 4 * 2^-23 < 5e-6 (the last term: exponentials of
+moves, and three additions of eight)."""
 
 import numpy as np
 import pytest
@@ -32,7 +37,9 @@ def _compare(tokens, logp, n, z, zd, x, n_draft, u, tau):
         lp = np.array(lp)
         assert np.array_equal(np.isnan(logp[i, :m]), np.isnan(lp))
         ok = ~np.isnan(lp)
-        assert np.all(np.abs(logp[i, :m] - lp)[ok] <= 2.0 ** -24 * np.abs(lp[ok]) + 1e-9)
+        sums = np.full(m, 1e-9 if zd is None else 5e-6)
+        sums[m - 1] = 1e-9
+        assert np.all(np.abs(logp[i, :m] - lp)[ok] <= (2.0 ** -24 * np.abs(lp) + sums)[ok])
 
 
 def _run(rbp, z, zd, x, n_draft, u, tau=1.0, dtype=torch.float32, pad=0):
@@ -121,6 +128,50 @@ def test_acceptance_at_the_border():
         u[i, 0] = (np.nextafter(r, np.float32(0)), r, np.nextafter(r, np.float32(2)))[i % 3]
     u = np.minimum(u, np.float32(1 - 2.0 ** -24))
     _run(rbp, z, zd, x, None, u)
+
+
+def test_acceptance_at_the_border_over_a_vocabulary():
+    """As above over 20001 tokens and through several drafts: the rough sums do not decide."""
+    rbp = require_gpu()
+    B, K, V = 8, 3, 20001
+    z, zd, x, u, _ = _case(B, K, V, torch.bfloat16, True, 4)
+    for i in range(B):
+        for k in range(K):
+            p, q = vocab.distribution(z[i, k]), vocab.distribution(zd[i, k])
+            r = np.float32(min(1.0, p[x[i, k]] / q[x[i, k]]))
+            u[i, k] = np.nextafter(r, np.float32(0)) if k < i % 3 else np.nextafter(r, np.float32(2))
+    u = np.minimum(u, np.float32(1 - 2.0 ** -24))
+    _run(rbp, z, zd, x, None, u, dtype=torch.bfloat16)
+
+
+def test_weights_left_by_a_draft_that_is_nearly_the_policy():
+    """p / q is 1 + 1e-6 and less on all tokens but the draft's: the rough sums do not know
+    which is larger, and the draw has to."""
+    rbp = require_gpu()
+    B, V = 12, 20001
+    rng = np.random.default_rng(21)
+    z = _values((B, 2, V), 1.0, torch.float32, rng)
+    x = np.argmin(z[:, :1], axis=2).astype(np.int32)
+    zd = z[:, :1].copy()
+    for i in range(B):  # masses of 1e-6 and more
+        zd[i, 0, x[i, 0]] += 1.0 + i / 4
+        if i % 3 == 0:
+            zd[i, 0, rng.integers(0, V, 300)] += 1.0
+    zd = torch.from_numpy(zd).float().double().numpy()
+    u = rng.random((B, 2)).astype(np.float32)
+    u[:, 0] = 0.99
+    _, _, n = _run(rbp, z, zd, x, None, u)
+    assert (n == 1).all()
+
+
+def test_nothing_left_of_an_identical_draft():
+    """A draft that is no token is rejected, and where the two rows are one (at other
+    alignments, so that their sums differ by roundings) the token is drawn from p."""
+    rbp = require_gpu()
+    z, _, _, u, _ = _case(9, 1, 5003, torch.float32, False, 22)
+    x = np.full((9, 1), -1, np.int32)
+    _, _, n = _run(rbp, z, z[:, :1].copy(), x, None, u)
+    assert (n == 1).all()
 
 
 def test_identical_draft_and_policy_accept_everything():

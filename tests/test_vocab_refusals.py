@@ -54,7 +54,7 @@ REFUSED = [
                                dict(tau=math.inf), dict(tau=math.nan), dict(tau=1e-38), dict(tau=1e38),
                                dict(z=ODD), dict(zd=ODD), dict(ws=ODD),
                                dict(typ=rbp.RBP_F32, z=ctypes.c_void_p(4098))]),
-    (_verify, rbp.RBP_EUNSUPPORTED, [dict(K=256), dict(B=1 << 23)]),
+    (_verify, rbp.RBP_EUNSUPPORTED, [dict(K=256), dict(B=1 << 23), dict(K=0, B=(1 << 21) + 1)]),
     (_verify, rbp.RBP_EWORKSPACE, [dict(ws=NULL), dict(ws_bytes=0)]),
     (_distill, rbp.RBP_EINVAL, [dict(z=NULL), dict(ids=NULL), dict(lt=NULL), dict(seq=NULL),
                                 dict(length=NULL), dict(kl=NULL), dict(loss=NULL),

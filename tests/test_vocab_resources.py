@@ -11,7 +11,8 @@ from test_kernel_resources import _kernels, pytestmark  # noqa: F401
     ("embed.hip", "embed_kernel"), ("embed.hip", "sort_one_kernel"),
     ("embed.hip", "sort_count_kernel"), ("embed.hip", "sort_scatter_kernel"),
     ("embed.hip", "run_sum_kernel"), ("embed.hip", "run_join_kernel"),
-    ("verify.hip", "stats_kernel"), ("verify.hip", "rest_kernel"), ("verify.hip", "finish_kernel"),
+    ("verify.hip", "stats_kernel"), ("verify.hip", "rough_kernel"), ("verify.hip", "exact_kernel"),
+    ("verify.hip", "finish_kernel"),
     ("distill.hip", "distill_row_kernel"), ("distill.hip", "distill_part_kernel"),
     ("distill.hip", "distill_join_kernel"), ("distill.hip", "distill_sum_kernel"),
 ])
