@@ -544,7 +544,7 @@ int rb_hist_accumulate(const int32_t* values, int64_t n, int32_t lo, int32_t n_b
  * out     device bf16 [T, d], overwritten.
  * Errors: RBP_EINVAL (null pointers, T < 0, d < 1, V < 1, scale not finite);
  *         RBP_EUNSUPPORTED (d % 8 != 0, table or out not aligned to 16 bytes,
- *         T above 2^31 - 1).
+ *         T above 2^31 - 1, T * d above 2^37 - 2^13).
  */
 int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
                      const int32_t* seq_of_token, int64_t T, int32_t d, int32_t V,
@@ -649,7 +649,7 @@ int policy_verify_drafts(const void* logits, const void* draft_logits, int logit
  * Errors: RBP_EINVAL (null pointers, T < 0, V < 1, K < 1, ld < V, B < 1, n_seq_total
  *         < 1, an unknown type, temperature outside [2^-100, 2^100], scale not
  *         finite, logits or dlogits not aligned to their type or ws to 16 bytes);
- *         RBP_EUNSUPPORTED (K above 256, T above 2^31 - 1); RBP_EWORKSPACE.
+ *         RBP_EUNSUPPORTED (K above 256, T of 2^22 or more); RBP_EWORKSPACE.
  */
 int policy_distill_fwd_bwd(const void* logits, int logits_type, int64_t ld,
                            const int32_t* teacher_ids, const float* teacher_logits,

@@ -143,7 +143,9 @@ __device__ __forceinline__ float mass_of(int32_t id, const int32_t* id_s, const 
 // pieces beyond them are read again for the gradient.  The first wave prepares
 // the teacher's entries while the row arrives.  An element that the teacher
 // names gets its gradient a second time, behind a barrier, so that the loop over
-// the row looks for nothing.
+// the row looks for nothing.  16384 x 152064 bf16 1.92 ms (5.2 TB/s), 1301 x 151936
+// fp32 317 us (5.0 TB/s, the pieces read twice not counted), 3003 x 151936 bf16
+// without a gradient 150 us (6.1 TB/s).
 template <class X, int kThreads, int kHold, bool kGrad, bool kBypass>
 __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz, Args a) {
   constexpr int E = Row<X>::E, kWaves = kThreads / 64;
@@ -625,7 +627,8 @@ extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64
               RBP_EINVAL, "policy_distill_fwd_bwd: need a temperature in [2^-100, 2^100] and a "
               "finite scale");
   RBP_REQUIRE(K <= kMaxK, RBP_EUNSUPPORTED, "policy_distill_fwd_bwd: K above %d", kMaxK);
-  RBP_REQUIRE(T <= INT32_MAX, RBP_EUNSUPPORTED, "policy_distill_fwd_bwd: T above 2^31 - 1");
+  // (a block of up to 1024 threads a token: less than 2^32 in all)
+  RBP_REQUIRE(T < (1 << 22), RBP_EUNSUPPORTED, "policy_distill_fwd_bwd: T of 2^22 or more");
   RBP_REQUIRE(loss_accum && stats && seq_len, RBP_EINVAL, "policy_distill_fwd_bwd: null pointer");
   if (T == 0) return RBP_OK;
   RBP_REQUIRE(logits && teacher_ids && teacher_logits && seq_of_token && kl, RBP_EINVAL,

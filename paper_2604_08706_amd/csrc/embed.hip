@@ -172,7 +172,7 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t total, uint32_t* wave_sum
   return lower;
 }
 
-// Up to kThreads * kItems tokens, in one block: every pass in LDS.
+// Up to kThreads * kItems tokens, in one block: every pass in LDS.  256 tokens 3.8 us.
 template <int kThreads, int kItems>
 __global__ void __launch_bounds__(kThreads) sort_one_kernel(
     const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int32_t T,
@@ -253,7 +253,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Keys in, int64
   hist[(int64_t)blockIdx.x * kBins + threadIdx.x] = bins[threadIdx.x];
 }
 
-// One pass: every key of the tile to its place.
+// One pass: every key of the tile to its place.  16384 tokens: 5 us, as the count
+// before it takes.
 template <int kItems>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
     Keys in, int64_t T, int shift, const uint32_t* __restrict__ hist, int n_tiles,
@@ -345,7 +346,8 @@ constexpr int kBatch = 4;  // rows of dx, and of dW, in flight
 
 // A group of kLanes lanes (8 columns each) per slice and kLanes * 8 columns.
 // part[slice][0]: the sum of the run that came in from the slice before,
-// part[slice][1]: of the run that begins here and goes on behind it.
+// part[slice][1]: of the run that begins here and goes on behind it.  16384 x 3584
+// fp32 added to 152064 rows: 91 us, 4.8 TB/s of dx and of the rows read and written.
 template <class X, int kLanes, bool kAdd>
 __global__ void __launch_bounds__(256) run_sum_kernel(const X* __restrict__ dx, Sorted in,
                                                       int n_chunks, int32_t d, int32_t V,
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const X* __restrict__ dx, 
 
 // The runs that cross slices, by a block for each slice that one begins in and chunk
 // of columns: its groups of lanes take equal stretches of the run's slices, and
-// the first adds their sums.
+// the first adds their sums: 6 us behind the above.
 template <int kLanes, bool kAdd>
 __global__ void __launch_bounds__(256) run_join_kernel(Sorted in, int n_chunks, int32_t d,
                                                        int32_t V, float scale,
@@ -540,9 +542,11 @@ extern "C" int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
   RBP_REQUIRE(aligned(table, 16) && aligned(out, 16), RBP_EUNSUPPORTED,
               "policy_embed_fwd: table and out must be aligned to 16 bytes");
   const int64_t n = T * (d / 8), blocks = rbp::ceil_div(n, 256 * kRowPieces);
-  RBP_REQUIRE(blocks <= INT32_MAX, RBP_EUNSUPPORTED, "policy_embed_fwd: T * d too large");
+  // (a launch has less than 2^32 threads)
+  RBP_REQUIRE(blocks < (1 << 24), RBP_EUNSUPPORTED, "policy_embed_fwd: T * d above 2^37 - 2^13");
   hipLaunchKernelGGL(n >= (1 << 19) ? embed_kernel<true> : embed_kernel<false>,
-                     dim3((unsigned)blocks), dim3(256), 0, rbp::as_stream(stream), table, tokens, seq_of_token, n, (uint32_t)(d / 8), V, scale, reinterpret_cast<uint4*>(out));
+                     dim3((unsigned)blocks), dim3(256), 0, rbp::as_stream(stream), table, tokens,
+                     seq_of_token, n, (uint32_t)(d / 8), V, scale, reinterpret_cast<uint4*>(out));
   RBP_CHECK_LAUNCH("policy_embed_fwd");
   return RBP_OK;
 }
@@ -578,10 +582,11 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   auto share = [&] {
     const int64_t from = n_fill * launch / n_launches, to = n_fill * (launch + 1) / n_launches;
     ++launch;
-    // (a few stores a thread: 545 MB 93 us with 4096 blocks, 86 so)
+    // (a few stores a thread: 545 MB 93 us with 4096 blocks, 86 so; more where the
+    // launch would have 2^32 threads)
     const int64_t blocks = rbp::ceil_div(to - from, kSortThreads * 4);
     return Fill{reinterpret_cast<float4*>(dW) + from, to - from,
-                (int)(blocks < (1 << 28) ? blocks : (1 << 28))};
+                (int)(blocks < (1 << 21) ? blocks : (1 << 21))};
   };
   if (T == 0) {
     const Fill f = share();

