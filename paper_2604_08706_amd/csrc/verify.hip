@@ -75,6 +75,11 @@ __constant__ double g_roots[kRoots] = {
     0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
     0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
     0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+__device__ __forceinline__ void load_roots(double* roots) {
+  const int i = threadIdx.x;
+  if (i < kRoots)
+    roots[i] = __hiloint2double(__double2hiint(g_roots[i]) - (i << 15), __double2loint(g_roots[i]));
+}
 struct Scaled {
   double p, root;  // their product is 2^(x k2 - c / 32)
 };
@@ -94,7 +99,11 @@ struct Grid {
     near = fabs(ref) * k2 < 0x1p24 && low > -1e30;
     floor = (float)low;
   }
-  // Exponentials of N logits: the roots' loads of all, then the polynomials.
+  // (fmaxf would quiet each operand first; a NaN may pass)
+  __device__ __forceinline__ void clamp(float& z) const {
+    asm("v_max_f32 %0, %1, %2" : "=v"(z) : "v"(z), "v"(floor));
+  }
+  // Exponentials of N clamped logits: the roots' loads of all, then the polynomials.
   template <int N>
   __device__ __forceinline__ void operator()(const float (&z)[N], const double* roots,
                                              Scaled (&y)[N]) const {
@@ -102,11 +111,8 @@ struct Grid {
     int n[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      // (fmaxf would quiet each operand first; a NaN may pass)
-      float x;
-      asm("v_max_f32 %0, %1, %2" : "=v"(x) : "v"(z[i]), "v"(floor));
-      const double t = fma((double)x, k, c);
-      f[i] = fma((double)x, k, c - t);
+      const double x = (double)z[i], t = fma(x, k, c);
+      f[i] = fma(x, k, c - t);
       n[i] = __double2loint(t);
       r[i] = roots[n[i] & (kRoots - 1)];
     }
@@ -120,12 +126,9 @@ struct Grid {
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      // the power of two goes into the exponent, which stays in range
-      int hi;
-      asm("v_lshl_add_u32 %0, %1, 15, %2"
-          : "=v"(hi)
-          : "v"(n[i] & ~(kRoots - 1)), "v"(__double2hiint(r[i])));
-      y[i].root = __hiloint2double(hi, __double2loint(r[i]));
+      // n / 32 goes into the exponent, which stays in range; what n % 32 adds below it
+      // is off the table's
+      y[i].root = __hiloint2double((n[i] << 15) + __double2hiint(r[i]), __double2loint(r[i]));
     }
   }
 };
@@ -134,6 +137,15 @@ __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
   return v;
+}
+
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+// The value of one lane, the same in all.
+__device__ __forceinline__ double lane_of(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                          __builtin_amdgcn_readlane(__double2loint(v), lane));
 }
 
 // s = sum of 2^((z - m) k2) over some logits; m = -inf and s = 0 for none but
@@ -294,7 +306,7 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
                                                               Args a, int64_t n_items) {
   constexpr int E = Row<X>::E, kBatch = 4;
   __shared__ double roots[kRoots];
-  if (threadIdx.x < kRoots) roots[threadIdx.x] = g_roots[threadIdx.x];
+  load_roots(roots);
   __syncthreads();
   const Place<X> place = place_of<false, X>(logits, nullptr, a, n_items);
   if (place.row == nullptr) return;
@@ -338,6 +350,8 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restric
     }
     double e[4] = {s, 0.0, 0.0, 0.0};  // sums of their own: no chain of 8 additions
     Scaled y[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) grid.clamp(x[i]);
     grid(x, roots, y);
 #pragma unroll
     for (int i = 0; i < E; ++i) e[i & 3] = fma(y[i].p, y[i].root, e[i & 3]);
@@ -542,11 +556,8 @@ __device__ void emit_accepted(const X* __restrict__ logits, const Args& a, int64
 template <class X>
 struct Weight {
   const X *p, *q;
-  double k2, mp, mq, lp, lq;
+  double mp, mq, lp, lq;
   int32_t kind, x;
-  __device__ __forceinline__ double rest(float zp, float zq) const {
-    return fmax(exp2_d(fma((double)zp - mp, k2, -lp)) - exp2_d(fma((double)zq - mq, k2, -lq)), 0.0);
-  }
 };
 template <class X>
 __device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logits,
@@ -554,7 +565,6 @@ __device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logit
   Weight<X> w;
   w.p = logits + (b * (a.K + 1) + d.accepted) * a.ld;
   w.q = d.kind == 2 ? draft_logits + (b * a.K + d.accepted) * a.ld_draft : nullptr;
-  w.k2 = a.k2;
   // (p itself is drawn from unnormalised, as its segments' sums are)
   w.mp = d.p.m;
   w.lp = d.kind == 2 ? d.p.ls : 0.0;
@@ -565,11 +575,20 @@ __device__ __forceinline__ Weight<X> weight_of(const Decision& d, const X* logit
   return w;
 }
 
+// Whether p > q by a decision's sums: z_p - z_q beyond this.
+__device__ __forceinline__ double rough_odds(const Decision& d, double k2) {
+  return (d.p.m - d.q.m) + (d.p.ls - d.q.ls) / k2;
+}
+// The root if `all`; else next to nothing, 2^-1042: its low word.
+__device__ __forceinline__ double some_of(double root, bool all) {
+  return __hiloint2double(all ? __double2hiint(root) : 0, __double2loint(root));
+}
+
 constexpr int kExactThreads = 512;
 
 // With draft logits: the decision, and the sums of the rows to draw from, a wave per
-// share of a segment.  64 sequences of 152064 tokens 25 us, 14 of them the 64-bit
-// operations at their rate (40 a token where both rows count), the rest the chain of
+// share of a segment.  64 sequences of 152064 tokens 20 us, 12 of them the 64-bit
+// operations at their rate (36 a token where both rows count), the rest the chain of
 // loads that decides.
 template <class X>
 __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restrict__ logits,
@@ -580,7 +599,7 @@ __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restric
   __shared__ DecideLds lds;
   __shared__ double roots[kRoots];
   constexpr int kWaves = kExactThreads / 64;
-  if (threadIdx.x < kRoots) roots[threadIdx.x] = g_roots[threadIdx.x];
+  load_roots(roots);
   const unsigned blocks = (a.segments * kShares + kWaves - 1) / kWaves;
   const int64_t b = blockIdx.x / blocks;
   const int32_t n = a.drafts(b);
@@ -607,14 +626,18 @@ __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restric
   const double mq = two ? d_s.q.m : d_s.p.m;
   gp.refer(d_s.p.m, a.k2, a.span);
   gq.refer(mq, a.k2, a.span);
+  gp.k = gq.k = lane_of(gp.k, 0);
   const bool near = gp.near && gq.near;
-  const double fp = near ? exp2_d(fma(-d_s.p.m, a.k2, gp.shift)) : 1.0;
-  const double fq = near ? exp2_d(fma(-mq, a.k2, gq.shift)) : 1.0;
-  // p > q by the rough sums
-  const double odds = fq * d_s.p.sum / (fp * d_s.q.sum);
+  const double fp = lane_of(near ? exp2_d(fma(-d_s.p.m, a.k2, gp.shift)) : 1.0, 0);
+  const double fq = lane_of(near ? exp2_d(fma(-mq, a.k2, gq.shift)) : 1.0, 0);
+  // p > q by the rough sums: z_p - z_q > c, and where that is off by 2^-22 |c| from its
+  // roundings or by kUnsure from the sums' the token is near
+  const float c0 = uniform((float)rough_odds(d_s, a.k2));
+  const float tol = uniform((float)(1.5 * kUnsure / a.k2 + 0x1p-22 * fabs((double)c0)));
+  const double odds = lane_of(d_s.p.sum / d_s.q.sum, 0);
   Drawn s{0.0, 0.0, 0.0, 0.0, 0.0};
-  auto add = [&](double p, double q, double o) {
-    const double d = fma(-q, o, p);
+  auto add = [&](double p, double q) {
+    const double d = fma(-q, odds, p);
     const bool larger = d > 0.0;
     s.p += p;
     s.q += q;
@@ -648,27 +671,46 @@ __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restric
         unpack(zp[0], p);
         if (two) unpack(zq[0], q);
         if (near) {
-          // four at a time: eight take registers that a second block needs
+          // four at a time, the policy's before the draft's: what that saves in registers
+          // a second block of the compute unit needs (72 -> 67 us in all)
 #pragma unroll
           for (int h = 0; h < E; h += 4) {
-            const float p4[4] = {p[h], p[h + 1], p[h + 2], p[h + 3]};
-            Scaled e[4], f[4];
+            float p4[4] = {p[h], p[h + 1], p[h + 2], p[h + 3]}, q4[4], d[4];
+            Scaled e[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              gp.clamp(p4[k]);
+              if (!two) continue;
+              q4[k] = q[h + k];
+              gq.clamp(q4[k]);
+              d[k] = (p4[k] - q4[k]) - c0;
+            }
             gp(p4, roots, e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s.p = fma(e[k].p, e[k].root, s.p);
             if (two) {
-              const float q4[4] = {q[h], q[h + 1], q[h + 2], q[h + 3]};
-              gq(q4, roots, f);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) add(e[k].p * e[k].root, f[k].p * f[k].root, odds);
-            } else {
+              for (int k = 0; k < 4; ++k)
+                s.a = fma(e[k].p, some_of(e[k].root, d[k] > 0.0f), s.a);
+              if (fminf(fminf(fabsf(d[0]), fabsf(d[1])), fminf(fabsf(d[2]), fabsf(d[3]))) < tol) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k) s.p = fma(e[k].p, e[k].root, s.p);
+                for (int k = 0; k < 4; ++k)
+                  if (fabsf(d[k]) < tol) s.near = fma(e[k].p, e[k].root, s.near);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+              gq(q4, roots, e);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                s.q = fma(e[k].p, e[k].root, s.q);
+                s.b = fma(e[k].p, some_of(e[k].root, d[k] > 0.0f), s.b);
+              }
             }
           }
         } else {
 #pragma unroll 1
           for (int k = 0; k < E; ++k) {
             add(exp2_d(((double)p[0] - d_s.p.m) * a.k2),
-                two ? exp2_d(((double)q[0] - d_s.q.m) * a.k2) : 0.0, odds);
+                two ? exp2_d(((double)q[0] - d_s.q.m) * a.k2) : 0.0);
 #pragma unroll
             for (int j = 1; j < E; ++j) p[j - 1] = p[j], q[j - 1] = q[j];
           }
@@ -682,15 +724,18 @@ __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restric
   const int32_t loose = r.loose(lane);
   if (share == 0 && loose >= 0 && (loose < r.head ? seg == 0 : seg == a.segments - 1))
     add(exp2_d(((double)value(rp[loose]) - d_s.p.m) * a.k2),
-        two ? exp2_d(((double)value(rq[loose]) - d_s.q.m) * a.k2) : 0.0,
-        d_s.p.sum / d_s.q.sum);
-  s.p = wave_sum(s.p);
-  if (two) {
-    s.q = wave_sum(s.q);
-    s.a = wave_sum(s.a);
-    s.b = wave_sum(s.b);
-    s.near = wave_sum(s.near);
-  }
+        two ? exp2_d(((double)value(rq[loose]) - d_s.q.m) * a.k2) : 0.0);
+  // four sums at once: each half of the wave goes on with two of them, each quarter
+  // with one
+  double x = lane < 32 ? s.p : s.q, y = lane < 32 ? s.a : s.b;
+  x += __shfl_xor(lane < 32 ? s.q : s.p, 32, 64);
+  y += __shfl_xor(lane < 32 ? s.b : s.a, 32, 64);
+  const double keep = lane & 16 ? y : x, give = lane & 16 ? x : y;
+  x = keep + __shfl_xor(give, 16, 64);
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
+  s.p = lane_of(x, 0), s.a = lane_of(x, 16), s.q = lane_of(x, 32), s.b = lane_of(x, 48);
+  if (__ballot(s.near != 0.0) != 0) s.near = wave_sum(s.near);
   if (lane == 0) a.drawn[b * a.segments * kShares + item] = s;
 }
 
@@ -737,12 +782,13 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
     __syncthreads();
     if (d_s.kind < 0) return;
     // The exact sums of both rows, and the segments' of max(p - q, 0).  The rough odds
-    // were off by `off`, so a segment's is by off times what lay near them at most: where
+    // were off by `off` and less, so a segment's is by off times what lay near them at most: where
     // that is more than 2^-30 of the total (u has steps of 2^-24) it is summed again.
     static_assert(kMaxSegments <= 64, "a lane per segment");
     if (wave == 0) {
       const double p = wave_sum(drawn.p), q = wave_sum(drawn.q);
-      const double off = fabs(d_s.p.sum * q / (d_s.q.sum * p) - 1.0);
+      const double off = fabs(d_s.p.sum * q / (d_s.q.sum * p) - 1.0) +
+                         0x1p-22 * fabs(rough_odds(d_s, a.k2)) * a.k2;
       const double rest = drawn.a / p - drawn.b / q;
       const double mine = rest > 0x1p-900 ? rest : 0.0;  // (2^-1000 a token may be nothing)
       const double total = wave_sum(mine);
@@ -815,12 +861,12 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
       for (;;) {
         const double mine = lane < a.segments ? seg_s[lane] : 0.0;
         scan = mine;
-#pragma unroll
+#pragma unroll 1
         for (int off = 1; off < 64; off <<= 1) {
           const double o = __shfl_up(scan, off, 64);
           if (lane >= off) scan += o;
         }
-        const double total = __shfl(scan, 63, 64);
+        const double total = lane_of(scan, 63);
         // (max(p - q, 0) below 2^-44 is the sums' rounding)
         if (total > (w.kind == 2 ? 0x1p-44 : 0.0) || w.kind == 0) {
           goal = u * total;
@@ -842,10 +888,9 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
     if (fixes == 0 && todo == 0 && last < 0 && some != 0)
       todo = 1ull << (63 - __builtin_clzll(some));
     if (fixes == 0 && todo == 0) break;
-    const int seg = __builtin_ctzll(fixes != 0 ? fixes : todo);
+    const int seg = __builtin_amdgcn_readfirstlane(__builtin_ctzll(fixes != 0 ? fixes : todo));
     const Segment<X> g(r, seg, a.log_segments);
-    double before = __shfl(scan, seg > 0 ? seg - 1 : 0, 64);
-    if (seg == 0) before = 0.0;
+    const double before = seg > 0 ? lane_of(scan, seg - 1) : 0.0;
     double sum = 0.0;
     bool done = false;
     for (int32_t v0 = g.v0; v0 < g.v1 && !done; v0 += kRun * kFinishThreads) {
@@ -877,7 +922,7 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
         for (int q = 1; q < kRun; ++q) zp[q - 1] = zp[q], zq[q - 1] = zq[q];
       }
       double upto = s;  // inclusive over the wave
-#pragma unroll
+#pragma unroll 1
       for (int off = 1; off < 64; off <<= 1) {
         const double o = __shfl_up(upto, off, 64);
         if (lane >= off) upto += o;
@@ -886,9 +931,9 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
       if (lane == 63) wave_s[wave] = upto;
       __syncthreads();
       double run = before + sum;
-#pragma unroll
+#pragma unroll 4
       for (int q = 0; q < kWaves; ++q) {
-        if (q < wave) run += wave_s[q];
+        run += q < wave ? wave_s[q] : 0.0;
         sum += wave_s[q];
       }
       if (fixes != 0) continue;
@@ -905,8 +950,8 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
       }
       // one atomic per wave (tokens ascend with the lanes): 1024 took 8 us
       const uint64_t hits = __ballot(hit < a.V), ends = __ballot(end >= 0);
-      if (hits != 0) hit = __shfl(hit, __builtin_ctzll(hits), 64);
-      if (ends != 0) end = __shfl(end, 63 - __builtin_clzll(ends), 64);
+      if (hits != 0) hit = __builtin_amdgcn_readlane(hit, __builtin_ctzll(hits));
+      if (ends != 0) end = __builtin_amdgcn_readlane(end, 63 - __builtin_clzll(ends));
       if (lane == 0 && hits != 0) atomicMin(&found, hit);
       if (lane == 0 && ends != 0) atomicMax(&last, end);
       __syncthreads();
