@@ -891,6 +891,7 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
     const int seg = __builtin_amdgcn_readfirstlane(__builtin_ctzll(fixes != 0 ? fixes : todo));
     const Segment<X> g(r, seg, a.log_segments);
     const double before = seg > 0 ? lane_of(scan, seg - 1) : 0.0;
+    const int terms = w.kind == 2 ? 2 : 1;
     double sum = 0.0;
     bool done = false;
     for (int32_t v0 = g.v0; v0 < g.v1 && !done; v0 += kRun * kFinishThreads) {
@@ -907,12 +908,14 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
 #pragma unroll 1
       for (int k = 0; k < kRun; ++k) {
         double wt = 0.0;
+        if (first + k < g.v1) {
 #pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-          const double y = i == 0 ? fma((double)zp[0] - w.mp, a.k2, -w.lp)
-                                  : fma((double)zq[0] - w.mq, a.k2, -w.lq);
-          const double e = exp2_d(y);
-          wt = i == 0 ? e : wt - e;
+          for (int i = 0; i < terms; ++i) {
+            const double y = i == 0 ? fma((double)zp[0] - w.mp, a.k2, -w.lp)
+                                    : fma((double)zq[0] - w.mq, a.k2, -w.lq);
+            const double e = exp2_d(y);
+            wt = i == 0 ? e : wt - e;
+          }
         }
         if (w.kind == 1 && first + k == w.x) wt = 0.0;
         wt = fmax(wt, 0.0);
