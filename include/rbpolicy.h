@@ -552,9 +552,10 @@ int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
 
 /*
  * Its backward: dW_v (+)= scale * sum over {t: tokens_t = v, not masked} of dx_t.
- * The tokens are sorted (stably) and each row's sum runs over its tokens in
- * batch order, in pieces of a fixed number of sorted positions: fp32, no
- * atomics on it, no dependence on how often a token occurs.
+ * Each row's sum runs over its tokens in batch order, in pieces that are then
+ * added in order: fp32, no atomics on it.  (Up to 512 tokens by blocks that look
+ * for equal ones; more are sorted, so that no time depends on how often a token
+ * occurs.)
  * dx      device [T, d], RBP_BF16 or RBP_F32 (dx_type); tokens, seq_of_token as in
  *         policy_embed_fwd (masked tokens and those outside [0, V) add nothing);
  * dW      device fp32 [V, d]: overwritten (rows without a token: 0), or added to

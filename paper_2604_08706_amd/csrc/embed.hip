@@ -6,7 +6,8 @@
 // values; the gradient reads T d values of dx and writes (or reads and writes)
 // the rows of dW that have a token, or all V rows when it overwrites.
 //
-// The gradient without atomics on floats: the tokens are sorted by id (stable
+// The gradient without atomics on floats: a few tokens' blocks look for tokens of
+// their id themselves (few_kernel); more tokens are sorted by id (stable
 // least-significant-digit radix sort of (id, position) pairs, up to 9 bits a
 // pass), so that a row's gradients are a run of sorted positions in batch order.
 // The sorted positions are cut into slices of equal length, whatever the tokens'
@@ -172,7 +173,7 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t total, uint32_t* wave_sum
   return lower;
 }
 
-// Up to kThreads * kItems tokens, in one block: every pass in LDS.  256 tokens 3.8 us.
+// Up to kThreads * kItems tokens, in one block: every pass in LDS.
 template <int kThreads, int kItems>
 __global__ void __launch_bounds__(kThreads) sort_one_kernel(
     const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int32_t T,
@@ -457,6 +458,107 @@ __global__ void __launch_bounds__(256) run_join_kernel(Sorted in, int n_chunks, 
   store8(o, scaled(kAdd ? load8(static_cast<const float*>(o)) : Row8{}, acc, scale));
 }
 
+// ---- few tokens -----------------------------------------------------------------
+
+// Up to kFewMost tokens in one launch, without a sort: a block per token and chunk of
+// columns marks the tokens of its id, goes on only if its own is the first of them,
+// and sums their rows, a group of lanes an equal stretch of them.  The blocks behind
+// clear the rows of dW that no token names, kFewFill float4 each.  Bound by latency:
+// 256 x 64 into 1024 rows 4.5 us against 12.4 of the three launches with a sort, 512 x
+// 3584 added 6.7 against 13.6.  A run is summed by one block for each of its chunks,
+// so 512 equal tokens take 23 against 14 (1024 would 43 against 19), and clearing
+// more than kFewClear is done sooner beside the sort (2.2 GB 379 against 391, but
+// 545 MB 102 against 99).
+constexpr int kFewMost = 512, kFewFill = 2048;
+constexpr int64_t kFewClear = 1 << 26;  // float4 of dW
+template <class X, int kLanes, bool kAdd>
+__global__ void __launch_bounds__(256) few_kernel(const X* __restrict__ dx,
+                                                  const int32_t* __restrict__ tokens,
+                                                  const int32_t* __restrict__ seq, int32_t T,
+                                                  int n_chunks, int32_t d, int32_t V, float scale,
+                                                  float* __restrict__ dW) {
+  constexpr int kGroups = 256 / kLanes, kTokens = kFewMost / 256, kWords = kFewMost / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t key[kTokens];
+#pragma unroll
+  for (int c = 0; c < kTokens; ++c)
+    key[c] = c * 256 + tid < T ? key_of(tokens, seq, c * 256 + tid, V) : kNoKey;
+  if (!kAdd && (int)blockIdx.x >= T * n_chunks) {
+    __shared__ uint8_t named[kFewFill];
+    const int32_t d4 = d / 4, rows = d4 < kFewFill ? kFewFill / d4 : 1;
+    const int64_t r0 = (int64_t)(blockIdx.x - T * n_chunks) * rows;
+    const int32_t n = (int32_t)(r0 + rows < V ? rows : V - r0);
+    for (int i = tid; i < n; i += 256) named[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < kTokens; ++c)
+      if (key[c] >= r0 && key[c] - r0 < n) named[key[c] - r0] = 1;
+    __syncthreads();
+    float4* o = reinterpret_cast<float4*>(dW) + r0 * d4;
+    for (uint32_t i = tid; i < (uint32_t)n * d4; i += 256)
+      if (!named[i / d4]) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    return;
+  }
+  __shared__ uint64_t word[kWords];
+  __shared__ uint16_t at_s[kFewMost];
+  __shared__ Row8 sum_s[kGroups][kLanes];
+  const int32_t t = blockIdx.x / n_chunks;
+  const uint32_t id = key_of(tokens, seq, t, V);
+  if (id >= (uint32_t)V) return;
+  bool on[kTokens];
+#pragma unroll
+  for (int c = 0; c < kTokens; ++c) {
+    on[c] = key[c] == id;
+    const uint64_t m = __ballot(on[c]);
+    if (lane == 0) word[c * 4 + wave] = m;
+  }
+  __syncthreads();
+  const uint64_t mine = lane < kWords ? word[lane] : 0;
+  const uint64_t below = lane < (t >> 6) ? ~0ull : lane == (t >> 6) ? (1ull << (t & 63)) - 1 : 0;
+  if (__ballot((mine & below) != 0) != 0) return;  // not the first (the same in every wave)
+  int upto = __popcll(mine);
+#pragma unroll
+  for (int off = 1; off < kWords; off <<= 1) {
+    const int o = __shfl_up(upto, off, 64);
+    if (lane >= off) upto += o;
+  }
+  const int m = __builtin_amdgcn_readlane(upto, kWords - 1);
+#pragma unroll
+  for (int c = 0; c < kTokens; ++c) {
+    const int w = c * 4 + wave;
+    const int before = w > 0 ? __builtin_amdgcn_readlane(upto, w - 1) : 0;
+    if (on[c])
+      at_s[before + __popcll(word[w] & ((1ull << lane) - 1))] = (uint16_t)(c * 256 + tid);
+  }
+  __syncthreads();
+  const int q = tid % kLanes, group = tid / kLanes;
+  const int32_t col = ((int32_t)(blockIdx.x % n_chunks) * kLanes + q) * 8;
+  const bool live = col < d;
+  const int each = (m + kGroups - 1) / kGroups, used = (m + each - 1) / each;
+  const int from = group * each, to = from + each < m ? from + each : m;
+  float* o = dW + (int64_t)id * d + col;
+  Row8 acc{}, old{};
+  if (kAdd && live && group == 0) old = load8(static_cast<const float*>(o));
+  if (live) {
+    for (int j = from; j < to; j += kBatch) {
+      Row8 r[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (j + i < to) r[i] = load8(dx + (int64_t)at_s[j + i] * d + col);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (j + i < to) add8(acc, r[i]);
+    }
+  }
+  if (used > 1) {
+    sum_s[group][q] = acc;
+    __syncthreads();
+  }
+  if (group != 0 || !live) return;
+  for (int g = 1; g < used; ++g) add8(acc, sum_s[g][q]);
+  store8(o, scaled(old, acc, scale));
+}
+
 __global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill<kSortThreads>(f, blockIdx.x); }
 
 // Keys per thread of a sort's tile: small tiles while their counts, which every tile
@@ -595,6 +697,30 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
     RBP_CHECK_LAUNCH("policy_embed_bwd");
     return RBP_OK;
   }
+  if (T <= kFewMost && n_fill <= kFewClear) {
+    with_lanes(d / 8, [&](auto lanes) {
+      constexpr int kLanes = decltype(lanes)::value;
+      const int n_chunks = (int)rbp::ceil_div(d / 8, kLanes);
+      const int32_t rows = d / 4 < kFewFill ? kFewFill / (d / 4) : 1;
+      const int64_t blocks = T * n_chunks + (accumulate_dW ? 0 : rbp::ceil_div(V, rows));
+      auto go = [&](auto kernel, auto* x) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, tokens, seq_of_token,
+                           (int32_t)T, n_chunks, d, V, scale, dW);
+      };
+      const auto* x32 = static_cast<const float*>(dx);
+      const auto* x16 = static_cast<const uint16_t*>(dx);
+      if (dx_type == RBP_F32 && accumulate_dW)
+        go(few_kernel<float, kLanes, true>, x32);
+      else if (dx_type == RBP_F32)
+        go(few_kernel<float, kLanes, false>, x32);
+      else if (accumulate_dW)
+        go(few_kernel<uint16_t, kLanes, true>, x16);
+      else
+        go(few_kernel<uint16_t, kLanes, false>, x16);
+    });
+    RBP_CHECK_LAUNCH("policy_embed_bwd");
+    return RBP_OK;
+  }
   const EmbedWs w = carve_embed(ws, T, d);
   const uint32_t *key = w.key[0], *at = w.at[0];
   if (one) {
@@ -605,9 +731,7 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
                          s, tokens, seq_of_token, V, (int32_t)T, passes, w.key[0], w.at[0], f);
     };
     using std::integral_constant;
-    if (T <= 512)
-      go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
-    else if (T <= 2048)
+    if (T <= 2048)
       go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
     else if (T <= 6144)
       go(integral_constant<int, 1024>{}, integral_constant<int, 6>{});

@@ -120,6 +120,16 @@ def test_gradient_types_widths_and_modes(T, d, V, dtype, acc):
     _check_backward(require_gpu(), T, d, V, "runs", dtype, acc, scale=-3.3)
 
 
+@pytest.mark.parametrize("acc", [False, True])
+@pytest.mark.parametrize("kind", ["one", "distinct", "runs", "skewed"])
+@pytest.mark.parametrize("T,d,V,dtype", [
+    (512, 520, 1025, torch.float32), (512, 8, 70001, torch.bfloat16), (511, 128, 3, torch.float32),
+    (5, 8200, 70, torch.bfloat16), (2, 256, 5000, torch.float32), (513, 128, 1000, torch.float32)])
+def test_gradient_of_few_tokens(T, d, V, dtype, kind, acc):
+    """Up to 512 tokens, summed without a sort, and the first count beyond them."""
+    _check_backward(require_gpu(), T, d, V, kind, dtype, acc, scale=0.7)
+
+
 def test_gradient_of_a_long_batch():
     """Many tiles of the sort and slices of the sums; half the batch is one token."""
     _check_backward(require_gpu(), 150001, 8, 5000, "skewed", torch.bfloat16, False, masked=False)

@@ -10,7 +10,7 @@ from test_kernel_resources import _kernels, pytestmark  # noqa: F401
 @pytest.mark.parametrize("src,kernel", [
     ("embed.hip", "embed_kernel"), ("embed.hip", "sort_one_kernel"),
     ("embed.hip", "sort_count_kernel"), ("embed.hip", "sort_scatter_kernel"),
-    ("embed.hip", "run_sum_kernel"), ("embed.hip", "run_join_kernel"),
+    ("embed.hip", "few_kernel"), ("embed.hip", "run_sum_kernel"), ("embed.hip", "run_join_kernel"),
     ("verify.hip", "stats_kernel"), ("verify.hip", "rough_kernel"), ("verify.hip", "exact_kernel"),
     ("verify.hip", "finish_kernel"),
     ("distill.hip", "distill_row_kernel"), ("distill.hip", "distill_part_kernel"),
