@@ -7,9 +7,10 @@
 // the rows of dW that have a token, or all V rows when it overwrites.
 //
 // The gradient without atomics on floats: a few tokens' blocks look for tokens of
-// their id themselves (few_kernel); more tokens are sorted by id (stable
-// least-significant-digit radix sort of (id, position) pairs, up to 9 bits a
-// pass), so that a row's gradients are a run of sorted positions in batch order.
+// their id themselves (few_kernel); more tokens are sorted by id, stably (thousands by
+// counting, beyond that by a least-significant-digit radix sort of (id, position)
+// pairs, up to 9 bits a pass), so that a row's gradients are a run of sorted positions
+// in batch order.
 // The sorted positions are cut into slices of equal length, whatever the tokens'
 // frequencies: a group of lanes walks a slice, sums runs in registers and writes
 // the runs that lie inside it; the ends of runs that cross a slice's border go to
@@ -91,6 +92,7 @@ __device__ __forceinline__ uint32_t key_of(const int32_t* __restrict__ tokens,
   const int32_t y = tokens[t];
   return (seq == nullptr || seq[t] >= 0) && y >= 0 && y < V ? (uint32_t)y : (uint32_t)V;
 }
+constexpr uint32_t kNoKey = 0xffffffffu;  // behind all of them
 __device__ __forceinline__ uint32_t digit_of(uint32_t key, int shift) {
   return (key >> shift) & (kBins - 1);
 }
@@ -173,54 +175,50 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t total, uint32_t* wave_sum
   return lower;
 }
 
-// Up to kThreads * kItems tokens, in one block: every pass in LDS.
-template <int kThreads, int kItems>
-__global__ void __launch_bounds__(kThreads) sort_one_kernel(
+// The sort of a few thousand tokens, in one launch: a block finds the places of kOwn of
+// them among all, by counting the keys that belong before each.  Its lanes are kOwn
+// tokens times stretches of the keys, which lie in LDS.
+constexpr int kRankThreads = 1024, kRankKeys = 12288;
+template <int kOwn>
+__global__ void __launch_bounds__(kRankThreads) rank_kernel(
     const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int32_t T,
-    int passes, uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
-  constexpr int kTile = kThreads * kItems, kWaves = kThreads / 64;
-  static_assert(kTile <= 65536 && kThreads >= kBins, "16-bit positions, a bin per thread");
-  __shared__ uint32_t cnt[kWaves + 1][kBins], base[kBins], wave_sum[kBins / 64];
-  __shared__ uint32_t key_s[kTile];
-  __shared__ uint16_t at_s[kTile];
-  if (blockIdx.x > 0) return fill<kThreads>(f, blockIdx.x - 1);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int i0 = wave * (64 * kItems) + lane, live = T - wave * (64 * kItems);
-  uint32_t key[kItems], at[kItems], place[kItems];
-#pragma unroll
-  for (int k = 0; k < kItems; ++k) {
-    at[k] = i0 + k * 64;
-    key[k] = (int)at[k] < T ? key_of(tokens, seq, at[k], V) : 0u;
+    uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
+  constexpr int kParts = kRankThreads / kOwn;
+  __shared__ uint4 key_s[kRankKeys / 4];
+  __shared__ uint32_t cnt_s[kParts][kOwn];
+  const int n_blocks = (T + kOwn - 1) / kOwn;
+  if ((int)blockIdx.x >= n_blocks) return fill<kRankThreads>(f, blockIdx.x - n_blocks);
+  uint32_t* keys = reinterpret_cast<uint32_t*>(key_s);
+  const int tid = threadIdx.x, own = tid % kOwn, part = tid / kOwn;
+  for (int i = tid; i < n_blocks * kOwn; i += kRankThreads)
+    keys[i] = i < T ? key_of(tokens, seq, i, V) : kNoKey;
+  __syncthreads();
+  const int i0 = blockIdx.x * kOwn;
+  const uint32_t mine = keys[i0 + own];
+  uint32_t cnt = 0;
+  // up to the block's own tokens equal keys come before, from there on smaller ones, and
+  // of its own the equal ones at lower positions
+  const int n4 = n_blocks * (kOwn / 4), j0 = n4 * part / kParts, j1 = n4 * (part + 1) / kParts;
+  const int mid = min(max(i0 / 4, j0), j1);
+#pragma unroll 4
+  for (int j = j0; j < mid; ++j) {
+    const uint4 k = key_s[j];
+    cnt += (k.x <= mine) + (k.y <= mine) + (k.z <= mine) + (k.w <= mine);
   }
-  for (int p = 0;; ++p) {
-    const int shift = p * kMaxDigit;
-    rank_tile<kItems, kWaves>(key, live, shift, cnt, place);
-    const uint32_t lower = scan_bins(tid < kBins ? cnt[kWaves][tid] : 0u, wave_sum);
-    if (tid < kBins) base[tid] = lower;
-    __syncthreads();
-    const bool last = p == passes - 1;
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      if (i0 + k * 64 >= T) continue;
-      const uint32_t digit = digit_of(key[k], shift);
-      const uint32_t to = base[digit] + cnt[wave][digit] + place[k];
-      if (last) {
-        key_out[to] = key[k];
-        at_out[to] = at[k];
-      } else {
-        key_s[to] = key[k];
-        at_s[to] = (uint16_t)at[k];
-      }
-    }
-    if (last) return;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kItems; ++k)
-      if (i0 + k * 64 < T) {
-        key[k] = key_s[i0 + k * 64];
-        at[k] = at_s[i0 + k * 64];
-      }
+#pragma unroll 4
+  for (int j = mid; j < j1; ++j) {
+    const uint4 k = key_s[j];
+    cnt += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
   }
+  for (int t = part; t < own; t += kParts) cnt += keys[i0 + t] == mine;
+  cnt_s[part][own] = cnt;
+  __syncthreads();
+  if (tid >= kOwn || i0 + tid >= T) return;
+  uint32_t to = 0;
+#pragma unroll 16
+  for (int k = 0; k < kParts; ++k) to += cnt_s[k][tid];
+  key_out[to] = mine;
+  at_out[to] = i0 + tid;
 }
 
 // Keys of a pass: the tokens' in the first, the previous pass's output later.
@@ -295,8 +293,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
 }
 
 // ---- sums over runs -------------------------------------------------------------
-
-constexpr uint32_t kNoKey = 0xffffffffu;
 
 struct Sorted {
   const uint32_t *key, *at;
@@ -564,11 +560,11 @@ __global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill<kSort
 // Keys per thread of a sort's tile: small tiles while their counts, which every tile
 // reads, stay few.
 inline int sort_items(int64_t T) { return T <= 65536 ? 2 : 8; }
-// Tokens that one block sorts: 6144, or 12288 beside the clearing of much of dW.  By
-// itself it takes 45 us for 16384, tiles on many units 19 in four launches; behind
-// 545 MB to be cleared (86 us) the one launch is the better (10007 tokens 114 us in
-// all against 134).
-constexpr int kOneMost = 6144, kOneBeside = 12288;
+// Tokens sorted in one launch, by counting, which takes their square: up to kRankMost
+// (4096 tokens of 896 bf16 17.8 us in all against 27.0 by tiles, 8192 27.9 / 30.4, 9000
+// 33.0 / 32.4), or all kRankKeys that fit beside the clearing of much of dW, which
+// hides it (10007 tokens, 545 MB 111 / 134).
+constexpr int kRankMost = 8192;
 constexpr int64_t kBesideFill = 1 << 24;  // float4 of dW
 
 // Positions per slice: enough slices to fill the chip (a group of lanes each, and
@@ -678,7 +674,7 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   const int passes = (bits + kMaxDigit - 1) / kMaxDigit;
   // dW's rows to be cleared, in equal shares behind each launch of the sort
   const int64_t n_fill = accumulate_dW ? 0 : (int64_t)V * (d / 4);
-  const bool one = T <= kOneMost || (T <= kOneBeside && n_fill >= kBesideFill);
+  const bool one = T <= kRankMost || (T <= kRankKeys && n_fill >= kBesideFill);
   const int n_launches = T == 0 || one ? 1 : 2 * passes;
   int launch = 0;
   auto share = [&] {
@@ -725,18 +721,21 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   const uint32_t *key = w.key[0], *at = w.at[0];
   if (one) {
     const Fill f = share();
-    auto go = [&](auto threads, auto items) {
-      constexpr int kThreads = decltype(threads)::value, kItems = decltype(items)::value;
-      hipLaunchKernelGGL((sort_one_kernel<kThreads, kItems>), dim3(1 + f.blocks), dim3(kThreads), 0,
-                         s, tokens, seq_of_token, V, (int32_t)T, passes, w.key[0], w.at[0], f);
+    auto go = [&](auto own) {
+      constexpr int kOwn = decltype(own)::value;
+      hipLaunchKernelGGL(rank_kernel<kOwn>, dim3((unsigned)(rbp::ceil_div(T, kOwn) + f.blocks)),
+                         dim3(kRankThreads), 0, s, tokens, seq_of_token, V, (int32_t)T, w.key[0],
+                         w.at[0], f);
     };
-    using std::integral_constant;
-    if (T <= 2048)
-      go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-    else if (T <= 6144)
-      go(integral_constant<int, 1024>{}, integral_constant<int, 6>{});
+    // Few tokens a block where many would leave units idle (4096 tokens 21.2 us in all
+    // with 64, 19.1 with 32, 17.8 with 16; 8192 30.8 / 27.9 with 64 and 32), many beside
+    // the clearing, which has use for the units (10007 tokens 111 us, 117 with 32).
+    if (n_fill >= kBesideFill)
+      go(std::integral_constant<int, 64>{});
+    else if (T <= 16 * 256)
+      go(std::integral_constant<int, 16>{});
     else
-      go(integral_constant<int, 1024>{}, integral_constant<int, 12>{});
+      go(std::integral_constant<int, 32>{});
   } else {
     auto go = [&](auto items) {
       constexpr int kItems = decltype(items)::value;

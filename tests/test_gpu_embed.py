@@ -168,11 +168,20 @@ def test_gradient_by_differences():
     assert difference == (dW.double() * step.double()).sum().item()  # small integers: exact
 
 
+@pytest.mark.parametrize("T,d,V,kind,acc", [
+    (4096, 24, 700, "runs", True), (8192, 16, 5000, "skewed", True), (8192, 8, 3, "distinct", True),
+    (8191, 8, 9000, "one", False), (12288, 448, 150001, "one", False),
+    (12287, 448, 150001, "skewed", False)])
+def test_gradient_sorted_by_counting(T, d, V, kind, acc):
+    """The most tokens of each rule, whole blocks and the last one short."""
+    _check_backward(require_gpu(), T, d, V, kind, torch.bfloat16, acc)
+
+
 @pytest.mark.parametrize("T,d,V,kind", [(7001, 448, 150001, "skewed"), (12289, 448, 150001, "runs"),
                                         (6145, 8, 511, "runs"), (20001, 24, 512, "skewed"),
                                         (600001, 8, 900, "runs")])
 def test_gradient_written_whole_on_every_route(T, d, V, kind):
-    """One block beside the clearing of dW; tiles with one, two and three digits; the longest
+    """Counting beside the clearing of dW; tiles with one, two and three digits; the longest
     slices."""
     _check_backward(require_gpu(), T, d, V, kind, torch.float32, False)
 

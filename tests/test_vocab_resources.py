@@ -8,7 +8,7 @@ from test_kernel_resources import _kernels, pytestmark  # noqa: F401
 
 
 @pytest.mark.parametrize("src,kernel", [
-    ("embed.hip", "embed_kernel"), ("embed.hip", "sort_one_kernel"),
+    ("embed.hip", "embed_kernel"), ("embed.hip", "rank_kernel"),
     ("embed.hip", "sort_count_kernel"), ("embed.hip", "sort_scatter_kernel"),
     ("embed.hip", "few_kernel"), ("embed.hip", "run_sum_kernel"), ("embed.hip", "run_join_kernel"),
     ("verify.hip", "stats_kernel"), ("verify.hip", "rough_kernel"), ("verify.hip", "exact_kernel"),
