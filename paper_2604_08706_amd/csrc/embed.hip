@@ -175,49 +175,61 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t total, uint32_t* wave_sum
   return lower;
 }
 
-// The sort of a few thousand tokens, in one launch: a block finds the places of kOwn of
-// them among all, by counting the keys that belong before each.  Its lanes are kOwn
-// tokens times stretches of the keys, which lie in LDS.
+// The sort of some thousand tokens, in one launch: a block finds the places of kOwn of
+// them among all, by counting the keys that belong before each.  A lane has kPer tokens,
+// for which it reads every kParts-th four of the keys from LDS (two: 8192 x 896 25.3 us
+// in all, 27.4 with one, 25.4 with four, which lose 0.5 us with fewer tokens).
 constexpr int kRankThreads = 1024, kRankKeys = 12288;
 template <int kOwn>
 __global__ void __launch_bounds__(kRankThreads) rank_kernel(
     const int32_t* __restrict__ tokens, const int32_t* __restrict__ seq, int32_t V, int32_t T,
     uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
-  constexpr int kParts = kRankThreads / kOwn;
+  constexpr int kPer = 2, kLanes = kOwn / kPer, kParts = kRankThreads / kLanes,
+                kWaves = kRankThreads / 64;
   __shared__ uint4 key_s[kRankKeys / 4];
-  __shared__ uint32_t cnt_s[kParts][kOwn];
+  __shared__ uint32_t cnt_s[kWaves][kOwn];
   const int n_blocks = (T + kOwn - 1) / kOwn;
   if ((int)blockIdx.x >= n_blocks) return fill<kRankThreads>(f, blockIdx.x - n_blocks);
   uint32_t* keys = reinterpret_cast<uint32_t*>(key_s);
-  const int tid = threadIdx.x, own = tid % kOwn, part = tid / kOwn;
+  const int tid = threadIdx.x, part = tid / kLanes;
   for (int i = tid; i < n_blocks * kOwn; i += kRankThreads)
     keys[i] = i < T ? key_of(tokens, seq, i, V) : kNoKey;
   __syncthreads();
-  const int i0 = blockIdx.x * kOwn;
-  const uint32_t mine = keys[i0 + own];
-  uint32_t cnt = 0;
+  const int i0 = blockIdx.x * kOwn, own = tid % kLanes * kPer;
+  uint32_t mine[kPer], cnt[kPer] = {};
+#pragma unroll
+  for (int p = 0; p < kPer; ++p) mine[p] = keys[i0 + own + p];
   // up to the block's own tokens equal keys come before, from there on smaller ones, and
   // of its own the equal ones at lower positions
-  const int n4 = n_blocks * (kOwn / 4), j0 = n4 * part / kParts, j1 = n4 * (part + 1) / kParts;
-  const int mid = min(max(i0 / 4, j0), j1);
-#pragma unroll 4
-  for (int j = j0; j < mid; ++j) {
+  const int n4 = n_blocks * (kOwn / 4);
+  int j = part;
+#pragma unroll 2
+  for (; j < i0 / 4; j += kParts) {
     const uint4 k = key_s[j];
-    cnt += (k.x <= mine) + (k.y <= mine) + (k.z <= mine) + (k.w <= mine);
+#pragma unroll
+    for (int p = 0; p < kPer; ++p)
+      cnt[p] += (k.x <= mine[p]) + (k.y <= mine[p]) + (k.z <= mine[p]) + (k.w <= mine[p]);
   }
-#pragma unroll 4
-  for (int j = mid; j < j1; ++j) {
+#pragma unroll 2
+  for (; j < n4; j += kParts) {
     const uint4 k = key_s[j];
-    cnt += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+#pragma unroll
+    for (int p = 0; p < kPer; ++p)
+      cnt[p] += (k.x < mine[p]) + (k.y < mine[p]) + (k.z < mine[p]) + (k.w < mine[p]);
   }
-  for (int t = part; t < own; t += kParts) cnt += keys[i0 + t] == mine;
-  cnt_s[part][own] = cnt;
+#pragma unroll
+  for (int p = 0; p < kPer; ++p) {
+    for (int t = part; t < own + p; t += kParts) cnt[p] += keys[i0 + t] == mine[p];
+#pragma unroll
+    for (int off = kLanes; off < 64; off <<= 1) cnt[p] += __shfl_xor(cnt[p], off, 64);
+    if ((tid & 63) < kLanes) cnt_s[tid >> 6][own + p] = cnt[p];
+  }
   __syncthreads();
   if (tid >= kOwn || i0 + tid >= T) return;
   uint32_t to = 0;
-#pragma unroll 16
-  for (int k = 0; k < kParts; ++k) to += cnt_s[k][tid];
-  key_out[to] = mine;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) to += cnt_s[w][tid];
+  key_out[to] = keys[i0 + tid];
   at_out[to] = i0 + tid;
 }
 
@@ -561,8 +573,8 @@ __global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill<kSort
 // reads, stay few.
 inline int sort_items(int64_t T) { return T <= 65536 ? 2 : 8; }
 // Tokens sorted in one launch, by counting, which takes their square: up to kRankMost
-// (4096 tokens of 896 bf16 17.8 us in all against 27.0 by tiles, 8192 27.9 / 30.4, 9000
-// 33.0 / 32.4), or all kRankKeys that fit beside the clearing of much of dW, which
+// (4096 tokens of 896 bf16 17.2 us in all against 27.0 by tiles, 8192 25.3 / 30.4, 10007
+// 34.5 / 34.0), or all kRankKeys that fit beside the clearing of much of dW, which
 // hides it (10007 tokens, 545 MB 111 / 134).
 constexpr int kRankMost = 8192;
 constexpr int64_t kBesideFill = 1 << 24;  // float4 of dW
