@@ -268,6 +268,19 @@ def test_logits_far_from_zero(drafted):
     _run(rbp, z, zd if drafted else None, x, None, u, 16.0, pad=1)
 
 
+@pytest.mark.parametrize("offset", [1e5, -3e6, 1e9])
+def test_draft_logits_far_from_the_policy_s(offset):
+    """The same distributions but for the offset's rounding (0.008, 0.25, 64): which of p and q
+    is larger does not show in 32-bit differences of logits."""
+    rbp = require_gpu()
+    B, K, V = 10, 2, 20001
+    z, zd, x, u, _ = _case(B, K, V, torch.float32, True, 61)
+    zd = (zd + offset).astype(np.float32).astype(np.float64)
+    u[::2, 0] = 1 - 2.0 ** -24
+    _run(rbp, z, zd, x, None, u)
+    _run(rbp, zd[:, [0, 1, 1]], z[:, :2], x, None, u, pad=1)
+
+
 @pytest.mark.parametrize("tau", [2.0 ** -100, 1e-3, 300.0, 1e30])
 def test_extreme_temperatures(tau):
     rbp = require_gpu()
