@@ -4,7 +4,9 @@ Trainer-side path of experience-replay RL for LLMs (arXiv 2604.08706): seeded
 replay-buffer sample-and-gather, per-token policy log-probabilities from final
 hidden states and the LM head (bf16 MFMA with an online log-sum-exp), the
 clipped importance-weighted GRPO loss with group advantages, and the backward
-to the hidden states and the LM head.  All compute is in librbpolicy.so
+to the hidden states and the LM head.  Beside it, at the same vocabulary: drafted
+tokens verified or sampled, the embedding and its gradient, distillation from a
+teacher's top logits.  All compute is in librbpolicy.so
 (hand-written HIP); this package is a thin binding over its C ABI
 (include/rbpolicy.h) and uses torch only for device memory and streams.
 """
