@@ -235,7 +235,7 @@ constexpr float kRoughSlack = 8.0f;
 // probabilities, |y| is at most log2 V + 2 kRoughSlack (the entropy bounds the distance
 // from the largest logit; the reference lags behind it, and moves), so the sum of a row
 // of 2^18 tokens is off by 5e-6 of itself at most, one of 2^31 by 7e-6, and p / q by
-// less than kUnsure.  Bound by HBM: 576 rows of 152064 bf16 33 us (5.3 TB/s).
+// less than kUnsure.  Bound by HBM: 576 rows of 152064 bf16 32 us (5.4 TB/s).
 constexpr double kUnsure = 0x1p-16;
 struct Rough {
   float m = -INFINITY;
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kStatsThreads) rough_kernel(const X* __restric
 }
 
 // A wave per segment of a row, in 64 bits: bound by its 13 64-bit operations a logit
-// and, with few rows, latency.  192 rows of 151936 fp32 23 us (5 TB/s), 5 of bf16 5 us.
+// and, with few rows, latency.  192 rows of 151936 fp32 21 us (5.5 TB/s), 5 of bf16 5 us.
 template <class X>
 __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const X* __restrict__ logits,
                                                               Args a, int64_t n_items) {
@@ -587,7 +587,7 @@ __device__ __forceinline__ double some_of(double root, bool all) {
 constexpr int kExactThreads = 512;
 
 // With draft logits: the decision, and the sums of the rows to draw from, a wave per
-// share of a segment.  64 sequences of 152064 tokens 20 us, 12 of them the 64-bit
+// share of a segment.  64 sequences of 152064 tokens 22 us, 13 of them the 64-bit
 // operations at their rate (36 a token where both rows count), the rest the chain of
 // loads that decides.
 template <class X>
@@ -739,7 +739,7 @@ __global__ void __launch_bounds__(kExactThreads) exact_kernel(const X* __restric
   if (lane == 0) a.drawn[b * a.segments * kShares + item] = s;
 }
 
-// A block per sequence: a chain of dependent loads and joins, 11 us for one sequence,
+// A block per sequence: a chain of dependent loads and joins, 9 us for one sequence,
 // 12 for 64.
 template <class X>
 __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restrict__ logits,
