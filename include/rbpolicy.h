@@ -610,8 +610,8 @@ int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
  * ws      device, >= rbp_workspace_bytes(RBP_OP_VERIFY, B, K, V).
  * Errors: RBP_EINVAL (null pointers, B < 0, K < 0, V < 1, ld or ld_draft < V, an
  *         unknown type, temperature outside [2^-100, 2^100], logits not aligned to
- *         their type or ws to 16 bytes); RBP_EUNSUPPORTED (K above 255, B above 2^21
- *         or B (K + 1) above 2^24); RBP_EWORKSPACE.
+ *         their type or ws to 16 bytes); RBP_EUNSUPPORTED (K above 255, B above 2^21,
+ *         B (K + 1) above 2^24 or V above 2^31 - 2^14 - 1); RBP_EWORKSPACE.
  */
 int policy_verify_drafts(const void* logits, const void* draft_logits, int logits_type,
                          int64_t ld, int64_t ld_draft, const int32_t* draft_tokens,
@@ -650,7 +650,8 @@ int policy_verify_drafts(const void* logits, const void* draft_logits, int logit
  * Errors: RBP_EINVAL (null pointers, T < 0, V < 1, K < 1, ld < V, B < 1, n_seq_total
  *         < 1, an unknown type, temperature outside [2^-100, 2^100], scale not
  *         finite, logits or dlogits not aligned to their type or ws to 16 bytes);
- *         RBP_EUNSUPPORTED (K above 256, T of 2^22 or more); RBP_EWORKSPACE.
+ *         RBP_EUNSUPPORTED (K above 256, T of 2^22 or more, V above 2^31 - 2^14 - 1);
+ *         RBP_EWORKSPACE.
  */
 int policy_distill_fwd_bwd(const void* logits, int logits_type, int64_t ld,
                            const int32_t* teacher_ids, const float* teacher_logits,

@@ -629,6 +629,8 @@ extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64
   RBP_REQUIRE(K <= kMaxK, RBP_EUNSUPPORTED, "policy_distill_fwd_bwd: K above %d", kMaxK);
   // (a block of up to 1024 threads a token: less than 2^32 in all)
   RBP_REQUIRE(T < (1 << 22), RBP_EUNSUPPORTED, "policy_distill_fwd_bwd: T of 2^22 or more");
+  RBP_REQUIRE(V <= rbp::rows::kMaxVocab, RBP_EUNSUPPORTED,
+              "policy_distill_fwd_bwd: V above 2^31 - 2^14 - 1");
   RBP_REQUIRE(loss_accum && stats && seq_len, RBP_EINVAL, "policy_distill_fwd_bwd: null pointer");
   if (T == 0) return RBP_OK;
   RBP_REQUIRE(logits && teacher_ids && teacher_logits && seq_of_token && kl, RBP_EINVAL,

@@ -1047,6 +1047,8 @@ extern "C" int policy_verify_drafts(const void* logits, const void* draft_logits
               "policy_verify_drafts: temperature must lie in [2^-100, 2^100]");
   RBP_REQUIRE(K <= 255 && B <= (1 << 21) && (int64_t)B * (K + 1) <= (1 << 24), RBP_EUNSUPPORTED,
               "policy_verify_drafts: K above 255, B above 2^21 or B (K + 1) above 2^24");
+  RBP_REQUIRE(V <= rbp::rows::kMaxVocab, RBP_EUNSUPPORTED,
+              "policy_verify_drafts: V above 2^31 - 2^14 - 1");
   if (B == 0) return RBP_OK;
   RBP_REQUIRE(logits && u && out_tokens && out_logp && n_out && (K == 0 || draft_tokens),
               RBP_EINVAL, "policy_verify_drafts: null pointer");

@@ -7,6 +7,11 @@
 namespace rbp {
 namespace rows {
 
+// The longest row that is taken.  Indices into a row are 32 bits wide and are compared with
+// its end after they have stepped over it: by a tile of verify.hip's search (5120 tokens) or a
+// block's threads, times the loads that are unrolled, at most 2^14 in all.
+constexpr int32_t kMaxVocab = INT32_MAX - (1 << 14);
+
 // A row of logits as 16-byte pieces: the pieces that lie whole and aligned in
 // it, and up to 2 (E - 1) elements before and behind them.
 template <class X>
