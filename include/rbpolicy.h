@@ -102,7 +102,9 @@ enum {
   RB_LAYOUT_PADDED = 1  /* one row of l_max tokens per draw                        */
 };
 
-/* ---- operations for rbp_workspace_bytes ------------------------------------ */
+/* ---- operations for rbp_workspace_bytes ------------------------------------
+ * Of RBP_OP_EMBED_BWD the size does not fall as n grows (d and V fixed): a workspace for the
+ * largest batch serves the smaller ones.                                       */
 enum {
   RBP_OP_SAMPLE_GATHER = 1, /* n = capacity of the record table              */
   RBP_OP_LOGPROB_FWD = 2,   /* n = T                                          */

@@ -16,6 +16,8 @@
 // the runs that lie inside it; the ends of runs that cross a slice's border go to
 // the workspace and are summed there, in order, by the group where the run begins.
 
+#include <algorithm>
+
 #include "logits_epilogue.h"
 #include "rbp_internal.h"
 
@@ -571,7 +573,8 @@ __global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill<kSort
 
 // Keys per thread of a sort's tile: small tiles while their counts, which every tile
 // reads, stay few.
-inline int sort_items(int64_t T) { return T <= 65536 ? 2 : 8; }
+constexpr int64_t kShortSort = 65536;
+inline int sort_items(int64_t T) { return T <= kShortSort ? 2 : 8; }
 // Tokens sorted in one launch, by counting, which takes their square: up to kRankMost
 // (4096 tokens of 896 bf16 17.2 us in all against 27.0 by tiles, 8192 25.3 / 30.4, 10007
 // 34.5 / 34.0), or all kRankKeys that fit beside the clearing of much of dW, which
@@ -581,10 +584,24 @@ constexpr int64_t kBesideFill = 1 << 24;  // float4 of dW
 
 // Positions per slice: enough slices to fill the chip (a group of lanes each, and
 // chunk of columns), few enough that a run over many slices is joined soon.
+constexpr int32_t kSliceLeast = 8, kSliceMost = 256, kSliceGroups = 4096;
 inline int32_t slice_of(int64_t T, int n_chunks) {
-  int32_t s = 8;
-  while (s < 256 && T * n_chunks > (int64_t)s * 4096) s *= 2;
+  int32_t s = kSliceLeast;
+  while (s < kSliceMost && T * n_chunks > (int64_t)s * kSliceGroups) s *= 2;
   return s;
+}
+
+// What a workspace provides for: at least the slices and tiles of T tokens, and no fewer for
+// more tokens (a longer batch may be cut into fewer of them), so that one sized for the largest
+// batch serves all.
+inline int64_t most_slices(int64_t T, int n_chunks) {
+  return std::min(rbp::ceil_div(T, kSliceLeast),
+                  std::max(rbp::ceil_div(T, kSliceMost), (int64_t)(kSliceGroups / n_chunks + 1)));
+}
+inline int64_t most_tiles(int64_t T) {
+  return T <= kShortSort ? rbp::ceil_div(T, kSortThreads * 2)
+                         : std::max(rbp::ceil_div(T, kSortThreads * 8),
+                                    rbp::ceil_div(kShortSort, kSortThreads * 2));
 }
 
 struct EmbedWs {
@@ -621,10 +638,9 @@ EmbedWs carve_embed(void* base, int64_t T, int32_t d) {
     w.key[k] = c.take<uint32_t>(n);
     w.at[k] = c.take<uint32_t>(n);
   }
-  const size_t tiles = (size_t)rbp::ceil_div(T, kSortThreads * sort_items(T));
-  w.hist = c.take<uint32_t>(tiles * kBins);
+  w.hist = c.take<uint32_t>((size_t)most_tiles(T) * kBins);
   const int32_t dd = d < 8 ? 8 : d;
-  w.part = c.take<float>((size_t)rbp::ceil_div(T, slice_of(T, chunks_of(dd))) * 2 * (size_t)dd);
+  w.part = c.take<float>((size_t)most_slices(T, chunks_of(dd)) * 2 * (size_t)dd);
   w.bytes = rbp::align_up(c.used, 256);
   return w;
 }

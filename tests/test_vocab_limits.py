@@ -1,6 +1,8 @@
 """The largest and the smallest that the embedding, verification and distillation take, and the
 sizes of their workspaces (CPU: the C ABI, stopped by its own checks before any launch)."""
 
+import random
+
 import pytest
 
 import paper_2604_08706_amd as rbp
@@ -16,3 +18,26 @@ def test_rows_whose_last_tile_passes_31_bits_are_refused(call):
     """Indices beyond the row's end are formed before they are compared with it."""
     assert call(LONGEST) == rbp.RBP_EWORKSPACE  # goes on to the next check
     assert call(LONGEST + 1) == call(2 ** 31 - 1) == rbp.RBP_EUNSUPPORTED
+
+
+def _growing(op, sizes, d, V):
+    """rbp_workspace_bytes over growing n."""
+    got = [rbp.rbp_workspace_bytes(op, n, d, V) for n in sizes]
+    for k in range(1, len(got)):
+        assert got[k] >= got[k - 1] > 0, (sizes[k - 1:k + 1], got[k - 1:k + 1], d, V)
+
+
+def _sizes(top, borders, seed):
+    """1 .. 300, both sides of every border, and others between, in order."""
+    rng = random.Random(seed)
+    sizes = set(range(1, 300)) | {round(top ** rng.random()) for _ in range(3000)}
+    for b in borders:
+        sizes |= {b - 1, b, b + 1}
+    return sorted(n for n in sizes if 1 <= n <= top)
+
+
+@pytest.mark.parametrize("d", [8, 64, 136, 512, 520, 896, 3584, 8200, 1 << 20])
+def test_embedding_gradient_workspace_grows_with_the_batch(d):
+    chunks = -(-d // 512) if d > 256 else 1
+    borders = [(8 << k) * 4096 // chunks for k in range(7)] + [512, 8192, 12288, 65536]
+    _growing(rbp.RBP_OP_EMBED_BWD, _sizes(1 << 27, borders, d), d, 152064)
