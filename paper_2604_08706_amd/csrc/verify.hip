@@ -23,6 +23,7 @@
 // bits --; 64-bit sums of the rows to draw from (exact), whose blocks decide first, an
 // acceptance too near for the rough sums by a 64-bit pass over its two rows; finish.
 
+#include <algorithm>
 #include <cmath>
 
 #include "rbp_internal.h"
@@ -981,12 +982,25 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
 // (32 with many rows: 576 rows of 152064 bf16 take 75 us in 64 segments, 68 in 32;
 // 5 rows 5.6 and 8.3); fewer where rows alone fill the chip many times over, since a
 // launch has less than 2^32 threads.
+constexpr int64_t kFewRows = 64, kFewItems = 1 << 20;
 int segments_of(int64_t B, int64_t K, int32_t V) {
   const int64_t rows = B * (2 * K + 1);
-  const int most = rows <= 64 ? kMaxSegments : kMaxSegments / 2;
+  const int most = rows <= kFewRows ? kMaxSegments : kMaxSegments / 2;
   int n = 1;
-  while (n < most && V / (2 * n) >= 512 && rows * n < (1 << 20)) n *= 2;
+  while (n < most && V / (2 * n) >= 512 && rows * n < kFewItems) n *= 2;
   return n;
+}
+
+// What a workspace provides for: at least the segments of `rows` rows in all, and no fewer for
+// more rows (which may be cut into fewer segments), so that one sized for the largest batch
+// serves all.
+int64_t most_items(int64_t rows, int32_t V) {
+  int64_t n = 1;  // of a row, but for the number of rows
+  while (n < kMaxSegments && V / (2 * n) >= 512) n *= 2;
+  const int64_t items =
+      rows <= kFewRows ? rows * n
+                       : std::max(kFewRows * n, rows * std::min<int64_t>(n, kMaxSegments / 2));
+  return std::min(items, std::max(2 * kFewItems, rows));
 }
 
 struct VerifyWs {
@@ -998,9 +1012,9 @@ struct VerifyWs {
 VerifyWs carve_verify(void* base, int64_t B, int64_t K, int32_t V) {
   rbp::WsCarver c(base);
   VerifyWs w;
-  const size_t segments = (size_t)segments_of(B, K, V);
-  w.parts = c.take<Part>((size_t)B * (2 * K + 1) * segments);
-  w.drawn = c.take<Drawn>((size_t)B * segments * kShares);
+  w.parts = c.take<Part>((size_t)most_items(B * (2 * K + 1), V));
+  // (with draft logits K is 1 or more, and its sequences have three rows or more)
+  w.drawn = c.take<Drawn>(K == 0 ? 0 : (size_t)rbp::ceil_div(most_items(3 * B, V), 3) * kShares);
   w.decisions = c.take<Decision>((size_t)B);
   w.bytes = rbp::align_up(c.used, 256);
   return w;

@@ -28,3 +28,34 @@ def test_embedding_gradients_of_many_sizes_in_the_workspace_of_the_largest():
         want = torch.zeros((V, d), dtype=torch.float64, device="cuda")
         want.index_add_(0, y[:T].long(), dx[:T].double())
         assert torch.equal(dW.double(), want)  # small integers: exact
+
+
+def test_verification_of_a_shrinking_batch_in_one_workspace():
+    """Sequences and drafts fall away: more segments a row from 64 rows on."""
+    rbp = require_gpu()
+    B, K, V = 40, 4, 33000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    z = torch.randn((B, K + 1, V), generator=g, device="cuda") * 2
+    zd = z[:, :K] + 0.5 * torch.randn((B, K, V), generator=g, device="cuda")
+    pick = torch.rand((B, K, V), generator=g, device="cuda").log_().neg_().log_().neg_()
+    x = (zd + pick).argmax(-1).int()
+    u = torch.rand((B, K + 1), generator=g, device="cuda")
+    ws = rbp.workspace(rbp.RBP_OP_VERIFY, B, K, V)
+    for b, k in ((40, 4), (21, 1), (8, 4), (7, 4), (1, 4), (32, 0), (3, 2)):
+        ws.fill_(255)
+        tokens = torch.empty((b, k + 1), dtype=torch.int32, device="cuda")
+        logp = torch.empty((b, k + 1), device="cuda")
+        n = torch.empty(b, dtype=torch.int32, device="cuda")
+        print(f"[workspace] verify B={b} K={k}", flush=True)
+        for draft in (zd, None):
+            zk = z[:b, :k + 1].contiguous()
+            dk = None if draft is None or k == 0 else draft[:b, :k].contiguous()
+            uk = u[:b, :k + 1].contiguous()
+            rbp.policy_verify_drafts(zk, dk, x[:b, :k].contiguous(), None, uk, tokens, logp, n, ws)
+            for i in (0, b - 1):
+                want, lp = vocab.verify(to_np(zk[i].double()),
+                                        None if dk is None else to_np(dk[i].double()),
+                                        to_np(x[i, :k]), k, to_np(uk[i]).astype(np.float64))
+                assert tokens[i, :len(want)].tolist() == want and n[i].item() == len(want)
+                assert np.abs(to_np(logp[i, :len(want)]) - lp).max() < 1e-5

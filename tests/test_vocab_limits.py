@@ -41,3 +41,17 @@ def test_embedding_gradient_workspace_grows_with_the_batch(d):
     chunks = -(-d // 512) if d > 256 else 1
     borders = [(8 << k) * 4096 // chunks for k in range(7)] + [512, 8192, 12288, 65536]
     _growing(rbp.RBP_OP_EMBED_BWD, _sizes(1 << 27, borders, d), d, 152064)
+
+
+VOCABULARIES = [1, 1000, 1024, 2047, 2048, 8192, 32768, 65536, 152064, 1 << 28]
+
+
+@pytest.mark.parametrize("V", VOCABULARIES)
+def test_verification_workspace_grows_with_sequences_and_drafts(V):
+    for K in (0, 1, 2, 4, 7, 31, 255):
+        rows = 2 * K + 1
+        borders = [64 // rows, 65 // rows] + [(1 << k) // rows for k in range(15, 25)]
+        _growing(rbp.RBP_OP_VERIFY, _sizes(min(1 << 21, (1 << 24) // (K + 1)), borders, V + K), K, V)
+    for B in (1, 2, 7, 8, 13, 21, 22, 63, 64, 65, 1000, 30000, 65536):
+        got = [rbp.rbp_workspace_bytes(rbp.RBP_OP_VERIFY, B, K, V) for K in range(256)]
+        assert all(a <= b for a, b in zip(got, got[1:])), (B, V)
