@@ -103,9 +103,9 @@ enum {
 };
 
 /* ---- operations for rbp_workspace_bytes ------------------------------------
- * Of RBP_OP_EMBED_BWD and RBP_OP_VERIFY the size does not fall as n grows, of
- * RBP_OP_VERIFY also not with d (the others fixed): a workspace for the largest
- * batch serves the smaller ones.                                               */
+ * Of RBP_OP_EMBED_BWD, RBP_OP_DISTILL and RBP_OP_VERIFY the size does not fall as
+ * n grows, of the last two also not with d (the others fixed): a workspace for the
+ * largest batch serves the smaller ones.                                       */
 enum {
   RBP_OP_SAMPLE_GATHER = 1, /* n = capacity of the record table              */
   RBP_OP_LOGPROB_FWD = 2,   /* n = T                                          */

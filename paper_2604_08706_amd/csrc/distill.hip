@@ -10,6 +10,8 @@
 // one block reads it into registers, reduces it with a running reference and sum
 // as it arrives, and writes the gradient from there.
 
+#include <algorithm>
+
 #include "rbp_internal.h"
 #include "vocab_rows.h"
 
@@ -564,10 +566,13 @@ void launch_rows(const X* z, X* dz, int64_t T, const Args& a, hipStream_t s) {
 // of long vocabularies (bf16, one block against shared: 1 x 151936 23.4 / 10.0 us,
 // 32 24.6 / 15.3, 64 25.1 / 20.6, 128 28.4 / 32.0; 1 x 16000 11.0 / 9.5, 64 x 16000
 // fp32 10.6 / 11.6).  The type does not enter: a workspace is sized without it.
+constexpr int64_t kFewRows = 64, kPartBlocks = 512, kRowElements = 512;
+constexpr int32_t kLongRow = 8192;
+constexpr int kMostParts = 64;
 int row_parts(int64_t T, int32_t V) {
   int parts = 1;
-  if (T <= 64 && V >= 8192 && V >= 512 * T)
-    while (parts < 64 && T * parts < 512 && V / (2 * parts) >= 2048) parts *= 2;
+  if (T <= kFewRows && V >= kLongRow && V >= kRowElements * T)
+    while (parts < kMostParts && T * parts < kPartBlocks && V / (2 * parts) >= 2048) parts *= 2;
   return parts;
 }
 
@@ -577,17 +582,20 @@ struct DistillWs {
   size_t bytes;
 };
 
+// Room for every batch of up to T rows, shared ones and others: one sized for the largest
+// batch serves all.
 DistillWs carve_distill(void* base, int64_t T, int32_t K, int32_t V) {
   rbp::WsCarver c(base);
   DistillWs d{};
   d.w.parts = row_parts(T, V);
-  if (d.w.parts == 1) {
-    d.terms = c.take<float>((size_t)T * 2);
-  } else {
-    d.w.A = c.take<double>((size_t)T);
-    d.w.stats = c.take<float2>((size_t)T * d.w.parts);
-    d.w.row = c.take<float2>((size_t)T);
-    d.w.p = c.take<float>((size_t)T * K);
+  d.terms = c.take<float>((size_t)T * 2);
+  const int64_t shared =
+      V < kLongRow ? 0 : std::min(std::min(T, kFewRows), (int64_t)V / kRowElements);
+  if (shared > 0) {
+    d.w.A = c.take<double>((size_t)shared);
+    d.w.stats = c.take<float2>((size_t)std::min(shared * kMostParts, 2 * kPartBlocks));
+    d.w.row = c.take<float2>((size_t)shared);
+    d.w.p = c.take<float>((size_t)shared * K);
   }
   d.bytes = rbp::align_up(c.used, 256);
   return d;

@@ -59,3 +59,29 @@ def test_verification_of_a_shrinking_batch_in_one_workspace():
                                         to_np(x[i, :k]), k, to_np(uk[i]).astype(np.float64))
                 assert tokens[i, :len(want)].tolist() == want and n[i].item() == len(want)
                 assert np.abs(to_np(logp[i, :len(want)]) - lp).max() < 1e-5
+
+
+def test_distillation_of_a_shrinking_batch_in_one_workspace():
+    """Rows shared by blocks from 64 on down, in the workspace of a batch that has none."""
+    rbp = require_gpu()
+    rng = np.random.default_rng(5)
+    T, V, K = 200, 33000, 100
+    ws = rbp.workspace(rbp.RBP_OP_DISTILL, T, K, V)
+    z = torch.from_numpy(rng.standard_normal((T, V)).astype(np.float32)).cuda()
+    ids = torch.from_numpy(rng.integers(0, V, (T, K)).astype(np.int32)).cuda()
+    lt = torch.from_numpy(rng.standard_normal((T, K)).astype(np.float32)).cuda()
+    seq = torch.zeros(T, dtype=torch.int32, device="cuda")
+    length = torch.ones(1, dtype=torch.int32, device="cuda")
+    for t in (200, 65, 64, 33, 16, 15, 1):
+        ws.fill_(255)
+        kl, loss, stats = (torch.zeros(n, device="cuda") for n in (t, 1, 2))
+        dz = torch.empty((t, V), device="cuda")
+        print(f"[workspace] distill T={t}", flush=True)
+        rbp.policy_distill_fwd_bwd(z[:t], ids[:t], lt[:t], None, seq[:t], length, 1, kl, loss, stats,
+                                   dz, ws)
+        rows = [0, t - 1]
+        wkl, _, _, wdz = vocab.distill(to_np(z[rows].double()), to_np(ids[rows]), to_np(lt[rows]),
+                                       None, [0, 0], [1], 1)
+        # KL terms of about 16 in fp32; gradients of exponentials off by 2^-24 (2 |y| + 4)
+        assert np.abs(to_np(kl[rows]) - wkl).max() < 2e-5 and stats[0].item() == t
+        assert np.abs(to_np(dz[rows]) - wdz).max() < 1e-6

@@ -55,3 +55,12 @@ def test_verification_workspace_grows_with_sequences_and_drafts(V):
     for B in (1, 2, 7, 8, 13, 21, 22, 63, 64, 65, 1000, 30000, 65536):
         got = [rbp.rbp_workspace_bytes(rbp.RBP_OP_VERIFY, B, K, V) for K in range(256)]
         assert all(a <= b for a, b in zip(got, got[1:])), (B, V)
+
+
+@pytest.mark.parametrize("V", VOCABULARIES)
+def test_distillation_workspace_grows_with_tokens_and_entries(V):
+    for K in (1, 8, 31, 256):
+        _growing(rbp.RBP_OP_DISTILL, _sizes((1 << 22) - 1, [64, V // 512], V + K), K, V)
+    for T in (1, 2, 15, 16, 17, 63, 64, 65, 300, 5000):
+        got = [rbp.rbp_workspace_bytes(rbp.RBP_OP_DISTILL, T, K, V) for K in range(1, 257)]
+        assert all(a <= b for a, b in zip(got, got[1:])), (T, V)
