@@ -35,6 +35,7 @@ struct Args {
   const int32_t *seq, *len;
   int32_t V, K;
   float inv_tau, weight;  // weight = scale / n_seq
+  double rtau;            // 1 / tau
   float *kl, *terms;      // terms: [T][2] loss term, 1 if the token counts
 };
 
@@ -65,18 +66,35 @@ struct Online {
   }
 };
 
+// Adding a constant to all logits changes no KL, but its parts log p, z / tau and lse each
+// have the constant's size: 32 bits would leave 3e-5 of a constant of 100.  So the teacher's
+// logits are taken relative to their largest before anything is rounded, and what the policy's
+// have in common cancels in 64 bits (an operation or two per entry).
+// (The logarithm of S is its exponent's and, in 32 bits, that of a number between 1/2 and 1:
+// to 2^-25 for a fraction of a 64-bit one's operations.)
+__device__ __forceinline__ double lse_of(float M, float S, double rtau) {
+  int e;
+  const float m = frexpf(S, &e);
+  return fma((double)M, rtau, fma((double)e, 0.69314718055994530942, (double)logf(m)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
 // The teacher's entries of a token, by one wave: entry k goes to id[k], p[k] (its
-// probability), y[k] (the policy's logit there) and e[k] = log p_k - y_k / tau;
-// up to a whole quarter of entries is filled with absent ones.
+// probability), lp[k] = log p_k and z[k] (the policy's logit there); up to a whole
+// quarter of entries is filled with absent ones.
 struct Teacher {
-  float P;   // sum of p
-  double A;  // sum of p e: KL = A + P lse
-  bool any;  // an entry of some mass (or a NaN)
+  float P;        // sum of p
+  double A, mass;  // sum of p (log p - z / tau), sum of p: KL = A + mass lse
+  bool any;       // an entry of some mass (or a NaN)
 };
 template <class X>
 __device__ __forceinline__ Teacher teacher_entries(const Args& a, int64_t t, const X* row,
                                                    int lane, int32_t* id_s, float* p_s,
-                                                   float* z_s, float* e_s) {
+                                                   float* z_s, float* lp_s) {
   constexpr int kPer = kMaxK / 64;
   int32_t id[kPer];
   float l[kPer];
@@ -88,42 +106,50 @@ __device__ __forceinline__ Teacher teacher_entries(const Args& a, int64_t t, con
     l[j] = -INFINITY;
     if (k < a.K) {
       id[j] = a.ids[t * a.K + k];
-      if (id[j] >= 0) l[j] = a.lt[t * a.K + k] * a.inv_tau;
+      if (id[j] >= 0) l[j] = a.lt[t * a.K + k];
     }
     top = fmaxf(top, l[j]);
     if (l[j] != l[j]) nan = 1.0f;
   }
   top = rbp::lp::wave_max(top);
   nan = rbp::lp::wave_max(nan);
-  float mass = 0.0f, P = 0.0f;
+  float P = 0.0f;
   if (a.mass != nullptr) {
-    mass = a.mass[t];
+    const double mass = (double)a.mass[t];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) l[j] = (float)((double)l[j] * a.rtau - mass);
   } else {
     float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) sum += id[j] >= 0 ? expf(l[j] - top) : 0.0f;
-    mass = top + logf(rbp::lp::wave_sum(sum));
+    for (int j = 0; j < kPer; ++j) {
+      l[j] = (l[j] - top) * a.inv_tau;
+      sum += id[j] >= 0 ? expf(l[j]) : 0.0f;
+    }
+    const float mass = logf(rbp::lp::wave_sum(sum));
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) l[j] -= mass;
   }
-  double A = 0.0;
+  double A = 0.0, mass = 0.0;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int k = j * 64 + lane;
-    const float logp = l[j] - mass, p = id[j] >= 0 ? expf(logp) : 0.0f;
+    const float p = id[j] >= 0 ? expf(l[j]) : 0.0f;
     P += p;
     if (k >= a.K) {
       if (k < ((a.K + 3) & ~3)) id_s[k] = -1, p_s[k] = 0.0f;
     } else {
       const float zk = id[j] >= 0 && id[j] < a.V ? value(row[id[j]]) : NAN;
-      const float e = logp - zk * a.inv_tau;
       id_s[k] = id[j];
       p_s[k] = p;
       z_s[k] = zk;
-      e_s[k] = e;
-      if (p != 0.0f) A += (double)p * (double)e;
+      lp_s[k] = l[j];
+      if (p != 0.0f) {
+        A += (double)p * ((double)l[j] - (double)zk * a.rtau);
+        mass += (double)p;
+      }
     }
   }
-  for (int off = 32; off >= 1; off >>= 1) A += __shfl_xor(A, off, 64);
-  return {rbp::lp::wave_sum(P), A, top > -INFINITY || nan > 0.0f};
+  return {rbp::lp::wave_sum(P), wave_sum(A), wave_sum(mass), top > -INFINITY || nan > 0.0f};
 }
 
 // The mass of an id over all entries that name it.
@@ -156,7 +182,7 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
   __shared__ int32_t any_s;
   __shared__ __attribute__((aligned(16))) int32_t id_s[kMaxK];
   __shared__ __attribute__((aligned(16))) float p_s[kMaxK];
-  __shared__ float z_s[kMaxK], e_s[kMaxK];
+  __shared__ float z_s[kMaxK], lp_s[kMaxK];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const X* row = z + t * a.ld;
@@ -202,7 +228,7 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
   const float edge = loose >= 0 ? value(row[loose]) : -INFINITY;
 
   if (wave == 0) {
-    const Teacher te = teacher_entries(a, t, row, lane, id_s, p_s, z_s, e_s);
+    const Teacher te = teacher_entries(a, t, row, lane, id_s, p_s, z_s, lp_s);
     if (lane == 0) {
       mass_s = te.P;
       any_s = te.any;
@@ -263,11 +289,12 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
   if (!any_s) return zeros();
   const float w = a.weight / (float)a.len[sq];
   if (wave == 0) {
-    const float lse = M * a.inv_tau + logf(S);
-    float kl = 0.0f;
+    const double lse = lse_of(M, S, a.rtau);
+    double sum = 0.0;
     for (int k = lane; k < a.K; k += 64)
-      if (p_s[k] != 0.0f) kl += p_s[k] * (e_s[k] + lse);
-    kl = rbp::lp::wave_sum(kl);
+      if (p_s[k] != 0.0f)
+        sum += (double)p_s[k] * ((double)lp_s[k] + (lse - (double)z_s[k] * a.rtau));
+    const float kl = (float)wave_sum(sum);
     if (lane == 0) {
       a.kl[t] = kl;
       a.terms[2 * t] = w * kl;
@@ -324,7 +351,7 @@ __global__ void __launch_bounds__(kThreads) distill_row_kernel(const X* z, X* dz
 constexpr int kPartThreads = 256;
 struct PartsWs {
   float2* stats;  // [T][parts] reference, sum
-  double* A;      // [T]
+  double2* A;     // [T] sum of p (log p - z / tau), sum of p
   float2* row;    // [T] P, 1 if the row counts
   float* p;       // [T][K]
   int parts;
@@ -345,7 +372,7 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(const X* __r
   constexpr int E = Row<X>::E, kWaves = kPartThreads / 64, kBatch = 4;
   __shared__ float2 s[kWaves];
   __shared__ int32_t id_s[kMaxK];
-  __shared__ float p_s[kMaxK], z_s[kMaxK], e_s[kMaxK];
+  __shared__ float p_s[kMaxK], z_s[kMaxK], lp_s[kMaxK];
   const int64_t t = blockIdx.x / w.parts;
   const int part = blockIdx.x % w.parts;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -376,10 +403,10 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(const X* __r
   const float2 mine = join(make_float2(o.m, o.s), 64, k2);
   if (lane == 0) s[wave] = mine;
   if (part == 0 && wave == kWaves - 1) {
-    const Teacher te = teacher_entries(a, t, row, lane, id_s, p_s, z_s, e_s);
+    const Teacher te = teacher_entries(a, t, row, lane, id_s, p_s, z_s, lp_s);
     for (int k = lane; k < a.K; k += 64) w.p[t * a.K + k] = p_s[k];
     if (lane == 0) {
-      w.A[t] = te.A;
+      w.A[t] = make_double2(te.A, te.mass);
       w.row[t] = make_float2(te.P, te.any ? 1.0f : 0.0f);
     }
   }
@@ -412,8 +439,7 @@ __global__ void __launch_bounds__(kPartThreads) distill_join_kernel(const X* z, 
       if (!in || i % w.parts != 0) continue;
       float kl = 0.0f;
       if (counts) {
-        kl = (float)(w.A[t] + (double)w.row[t].x *
-                                  ((double)(all.x * a.inv_tau) + (double)logf(all.y)));
+        kl = (float)(w.A[t].x + w.A[t].y * lse_of(all.x, all.y, a.rtau));
         v[0] += a.weight / (float)a.len[a.seq[t]] * kl;
         v[1] += 1.0;
         v[2] += kl;
@@ -592,7 +618,7 @@ DistillWs carve_distill(void* base, int64_t T, int32_t K, int32_t V) {
   const int64_t shared =
       V < kLongRow ? 0 : std::min(std::min(T, kFewRows), (int64_t)V / kRowElements);
   if (shared > 0) {
-    d.w.A = c.take<double>((size_t)shared);
+    d.w.A = c.take<double2>((size_t)shared);
     d.w.stats = c.take<float2>((size_t)std::min(shared * kMostParts, 2 * kPartBlocks));
     d.w.row = c.take<float2>((size_t)shared);
     d.w.p = c.take<float>((size_t)shared * K);
@@ -653,7 +679,8 @@ extern "C" int policy_distill_fwd_bwd(const void* logits, int logits_type, int64
   hipStream_t s = rbp::as_stream(stream);
   const DistillWs d = carve_distill(ws, T, K, V);
   const Args a{ld, teacher_ids, teacher_logits, teacher_lse, seq_of_token, seq_len, V, K,
-               1.0f / temperature, (float)((double)scale / (double)n_seq_total), kl, d.terms};
+               1.0f / temperature, (float)((double)scale / (double)n_seq_total),
+               1.0 / (double)temperature, kl, d.terms};
   auto go = [&](auto type) {
     using X = decltype(type);
     const X* z = static_cast<const X*>(logits);

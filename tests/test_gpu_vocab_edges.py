@@ -85,3 +85,41 @@ def test_distillation_of_a_shrinking_batch_in_one_workspace():
         # KL terms of about 16 in fp32; gradients of exponentials off by 2^-24 (2 |y| + 4)
         assert np.abs(to_np(kl[rows]) - wkl).max() < 2e-5 and stats[0].item() == t
         assert np.abs(to_np(dz[rows]) - wdz).max() < 1e-6
+
+
+@pytest.mark.parametrize("shift", [100.0, -1000.0, 30000.0])
+@pytest.mark.parametrize("tau", [1.0, 0.7])
+@pytest.mark.parametrize("T,V", [(70, 3000), (3, 20000)])
+@pytest.mark.parametrize("use_mass", [False, True])
+def test_divergence_does_not_depend_on_a_constant_in_the_logits(T, V, tau, shift, use_mass):
+    """All values are multiples of 2^-7 below 2^15, so that the shifted ones are exact.  An
+    exponential of y - max is off by 2^-24 (2 |y - max| + 4), a sum of positive terms in pieces by
+    (V / 64 + 64) of them, the teacher's part likewise, wherever the logits lie; a teacher's sum
+    that is given is taken as it is.  Blocks of their own and rows shared by blocks."""
+    rbp = require_gpu()
+    rng = np.random.default_rng(int(V + abs(shift)))
+    K = 9
+    z = np.round(rng.standard_normal((T, V)) * 2 * 128) / 128
+    lt = np.round((rng.standard_normal((T, K)) * 2 + 6) * 128) / 128
+    ids = rng.integers(0, V, (T, K)).astype(np.int32)
+    tau = float(np.float32(tau))
+    # (multiples of 128 over tau would not be exact: the sum is shifted in 64 bits, rounded once)
+    mass = np.log(np.exp(lt / tau).sum(1)) + 0.5 + shift / tau if use_mass else None
+    mass = None if mass is None else mass.astype(np.float32)
+    z, lt = z + shift, lt + shift
+    assert np.array_equal(z.astype(np.float32), z) and np.array_equal(lt.astype(np.float32), lt)
+    kl, loss, stats = (torch.zeros(n, device="cuda") for n in (T, 1, 2))
+    rbp.policy_distill_fwd_bwd(
+        torch.from_numpy(z).float().cuda(), torch.from_numpy(ids).cuda(),
+        torch.from_numpy(lt).float().cuda(), None if mass is None else torch.from_numpy(mass).cuda(),
+        torch.zeros(T, dtype=torch.int32, device="cuda"),
+        torch.ones(1, dtype=torch.int32, device="cuda"), 1, kl, loss, stats, None,
+        rbp.workspace(rbp.RBP_OP_DISTILL, T, K, V), temperature=tau)
+    wkl, wloss, _, _ = vocab.distill(z, ids, lt, mass, [0] * T, [1], 1, tau)
+    spread = (z.max() - z.min() + lt.max() - lt.min()) / tau
+    P = 1.0 if mass is None else \
+        np.exp((lt - lt.max()) / tau + (lt.max() / tau - mass[:, None].astype(np.float64))).sum(1)
+    # its exponentials, its sum, and the roundings of what is left, below 2 spread + 16
+    tol = P * 2.0 ** -24 * (2 * spread + 4 + V / 64 + 64 + 4 * (2 * spread + 16))
+    assert np.all(np.abs(to_np(kl) - wkl) <= tol)
+    assert abs(loss.item() - wloss) <= np.sum(tol) + 2.0 ** -22 * abs(wloss)
