@@ -123,3 +123,43 @@ def test_divergence_does_not_depend_on_a_constant_in_the_logits(T, V, tau, shift
     tol = P * 2.0 ** -24 * (2 * spread + 4 + V / 64 + 64 + 4 * (2 * spread + 16))
     assert np.all(np.abs(to_np(kl) - wkl) <= tol)
     assert abs(loss.item() - wloss) <= np.sum(tol) + 2.0 ** -22 * abs(wloss)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("off,pad", [(1, 0), (3, 0), (0, 3), (2, 5)])
+def test_shared_rows_with_a_gradient_aligned_unlike_its_logits(dtype, off, pad):
+    """Few long rows, whose blocks then store element by element: the bits of an aligned gradient,
+    and nothing beside it."""
+    rbp = require_gpu()
+    rng = np.random.default_rng(off + pad)
+    T, V, K = 5, 9001, 7
+    z = torch.from_numpy(rng.standard_normal((T, V))).to(dtype).cuda()
+    ids = torch.from_numpy(rng.integers(0, V, (T, K)).astype(np.int32)).cuda()
+    ids[:, 0], ids[:, 1] = 0, V - 1  # loose elements of the row's ends
+    lt = torch.from_numpy(rng.standard_normal((T, K)).astype(np.float32)).cuda()
+    seq = torch.tensor([0, 0, -1, 0, 0], dtype=torch.int32, device="cuda")
+    length = torch.ones(1, dtype=torch.int32, device="cuda")
+    ws = rbp.workspace(rbp.RBP_OP_DISTILL, T, K, V)
+
+    def call(logits, dz):
+        kl, loss, stats = (torch.zeros(n, device="cuda") for n in (T, 1, 2))
+        rbp.policy_distill_fwd_bwd(logits, ids, lt, None, seq, length, 1, kl, loss, stats, dz, ws)
+        return kl
+
+    # rows at one place of 16 bytes each in the logits; the gradient `off` elements on
+    wide = torch.full((T, V + pad), float("nan"), dtype=dtype, device="cuda")
+    wide[:, :V] = z
+    want = torch.empty((T, V + pad), dtype=dtype, device="cuda")
+    kl = call(wide[:, :V], want[:, :V])
+    flat = torch.full((off + T * (V + pad) + 8,), 7.0, dtype=dtype, device="cuda")
+    dz = flat[off:off + T * (V + pad)].view(T, V + pad)
+    print(f"[shared] {dtype} off={off} pad={pad}", flush=True)
+    assert torch.equal(call(wide[:, :V], dz[:, :V]), kl)
+    assert torch.equal(dz[:, :V], want[:, :V])
+    assert dz[:, V:].eq(7).all() and flat[:off].eq(7).all() and flat[off + T * (V + pad):].eq(7).all()
+    _, _, _, exact = vocab.distill(to_np(z.double()), to_np(ids), to_np(lt), None, to_np(seq), [1], 1)
+    half = 0.0 if dtype == torch.float32 else 2.0 ** -8
+    # exponentials off by 2^-24 (2 |y| + 4) of themselves and sums by 2^-24 (V / 64 + 64), beside
+    # the teacher's probabilities of at most 1
+    assert np.all(np.abs(to_np(dz[:, :V].double()) - exact)
+                  <= half * np.abs(exact) + 2.0 ** -24 * 300 * (np.abs(exact) + (exact < 0)))
