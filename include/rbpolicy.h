@@ -602,10 +602,12 @@ int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
  * n_out   device int32 [B]: tokens emitted, a + 1.
  * Comparisons, the search for the drawn token and the sums that decide are in 64 bits,
  * so a decision differs from the exact one only where a border lies within about
- * 1e-12 of u (2^-25, half a step of u, where a token is drawn from max(p_a - q_a, 0)).
+ * 1e-12 of u.  Where a token is drawn from max(p_a - q_a, 0), whose total R is a
+ * difference of such sums, that is within 2^-25 (half a step of u) + 1e-12 / R; and
+ * a total of 2^-36 or less counts as 0 (such a rejection has that probability).
  * out_logp beside draft_logits comes from 32-bit sums for accepted drafts (off by at
- * most 5e-6 at V = 2^18), from 64-bit ones else.  Weights max(p_a - q_a, 0) whose total
- * is below 2^-44 count as all 0.  Logits of -infinity have probability 0.  A row of logits with a NaN,
+ * most 5e-6 at V = 2^18), from 64-bit ones else.
+ * Logits of -infinity have probability 0.  A row of logits with a NaN,
  * with +infinity, or with -infinity only has no distribution: a draft at such a
  * position of the policy's is rejected, and drawing there emits token -1 with a
  * NaN log-prob; such a row of draft_logits has its draft rejected, and the token

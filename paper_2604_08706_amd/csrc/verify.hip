@@ -413,6 +413,9 @@ __device__ __forceinline__ Dist dist_of(const Part* parts, int n, double k2, int
 
 constexpr int kMaxK = 255;
 constexpr int kShares = 2;  // waves of a segment in exact_kernel
+// A total of max(p - q, 0) that counts as 0.  It is a difference of sums whose exponentials are
+// off by 8e-14, so by 4e-13 at most; above this, by 3 in a hundred of itself at most.
+constexpr double kNothing = 0x1p-36;
 constexpr int kFinishThreads = 1024;
 constexpr int kRun = 5;  // tokens of a thread: a segment of 152064 / 32 in one tile
 constexpr int kMaxSegments = 64;
@@ -784,7 +787,8 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
     if (d_s.kind < 0) return;
     // The exact sums of both rows, and the segments' of max(p - q, 0).  The rough odds
     // were off by `off` and less, so a segment's is by off times what lay near them at most: where
-    // that is more than 2^-30 of the total (u has steps of 2^-24) it is summed again.
+    // that is more than 2^-31 of the total it is summed again, so that 64 segments are off by
+    // 2^-25 of it together, half a step of u.
     static_assert(kMaxSegments <= 64, "a lane per segment");
     if (wave == 0) {
       const double p = wave_sum(drawn.p), q = wave_sum(drawn.q);
@@ -794,7 +798,7 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
       const double mine = rest > 0x1p-900 ? rest : 0.0;  // (2^-1000 a token may be nothing)
       const double total = wave_sum(mine);
       if (lane < a.segments) seg_s[lane] = mine;
-      const uint64_t fixes = __ballot(off * drawn.near > 0x1p-30 * total * p);
+      const uint64_t fixes = __ballot(off * drawn.near > 0x1p-31 * total * p);
       if (lane == 0) {
         fixes_s = fixes;
         d_s.p.sum = p;
@@ -868,8 +872,7 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const X* __restr
           if (lane >= off) scan += o;
         }
         const double total = lane_of(scan, 63);
-        // (max(p - q, 0) below 2^-44 is the sums' rounding)
-        if (total > (w.kind == 2 ? 0x1p-44 : 0.0) || w.kind == 0) {
+        if (total > (w.kind == 2 ? kNothing : 0.0) || w.kind == 0) {
           goal = u * total;
           some = __ballot(mine > 0.0);
           todo = __ballot(mine > 0.0 && scan > goal);

@@ -163,3 +163,64 @@ def test_shared_rows_with_a_gradient_aligned_unlike_its_logits(dtype, off, pad):
     # the teacher's probabilities of at most 1
     assert np.all(np.abs(to_np(dz[:, :V].double()) - exact)
                   <= half * np.abs(exact) + 2.0 ** -24 * 300 * (np.abs(exact) + (exact < 0)))
+
+
+def _verify_one_draft(rbp, z, zd, x, u):
+    """Tokens emitted first, and their number, of one fp32 draft per row of z [B, 2, V]."""
+    B, _, V = z.shape
+    tokens = torch.empty((B, 2), dtype=torch.int32, device="cuda")
+    logp, n = torch.empty((B, 2), device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    rbp.policy_verify_drafts(torch.from_numpy(z).float().cuda(), torch.from_numpy(zd).float().cuda(),
+                             torch.from_numpy(x).cuda(), None, torch.from_numpy(u).cuda(), tokens,
+                             logp, n, rbp.workspace(rbp.RBP_OP_VERIFY, B, 1, V))
+    return to_np(tokens)[:, 0], to_np(n)
+
+
+def test_draws_from_a_small_remainder_beside_the_borders_of_segments():
+    """Totals of max(p - q, 0) around 1e-7: the drawn token's step of the exact running sum holds u
+    but for 2^-25 + 1e-12 / total, which the header states.  (64 segments of a row: the borders
+    between them and their neighbours, where a segment's error would show.)"""
+    rbp = require_gpu()
+    rng = np.random.default_rng(11)
+    B, V = 20, 70001
+    z = rng.standard_normal((B, 2, V)).astype(np.float32).astype(np.float64)
+    zd, x = z[:, :1].copy(), np.zeros((B, 1), np.int32)
+    u = np.full((B, 2), 0.99, np.float32)
+    run = []
+    for i in range(B):
+        x[i, 0] = rng.integers(0, V)
+        z[i, 0, x[i, 0]] = zd[i, 0, x[i, 0]] = -2.0
+        zd[i, 0, x[i, 0]] += 0.05 * (1 + i % 4)
+        e = [np.exp(a.astype(np.longdouble)) for a in (z[i, 0], zd[i, 0])]
+        rest = np.maximum(e[0] / e[0].sum() - e[1] / e[1].sum(), 0)
+        run.append((np.cumsum(rest / rest.sum()), float(rest.sum())))
+        at = (V * int(rng.integers(1, 64))) // 64 + i % 3 - 1
+        u[i, 1] = np.float32(run[i][0][at])
+    tokens, n = _verify_one_draft(rbp, z, zd, x, u)
+    assert (n == 1).all()
+    for i, (cdf, total) in enumerate(run):
+        assert 1e-8 < total < 1e-6 and tokens[i] != x[i, 0]
+        off = 2.0 ** -25 + 1e-12 / total
+        low = cdf[tokens[i] - 1] if tokens[i] > 0 else 0
+        assert low - off <= u[i, 1] <= cdf[tokens[i]] + off, (i, total)
+
+
+def test_a_remainder_below_the_sums_own_error_counts_as_none():
+    """One fp32 step more at the draft's logit leaves about 1e-12, a few times what the two sums are
+    off by: the token is drawn from p, so with u inside the draft's own step it is the draft's."""
+    rbp = require_gpu()
+    rng = np.random.default_rng(12)
+    B, V = 8, 20001
+    z = rng.standard_normal((B, 2, V)).astype(np.float32)
+    zd, x = z[:, :1].copy(), rng.integers(0, V, (B, 1)).astype(np.int32)
+    u = np.full((B, 2), 1 - 2.0 ** -24, np.float32)
+    for i in range(B):
+        z[i, 0, x[i, 0]] = zd[i, 0, x[i, 0]] = -1.5
+        zd[i, 0, x[i, 0]] = np.nextafter(np.float32(-1.5), np.float32(0))
+        p = vocab.distribution(z[i, 0].astype(np.float64))
+        q = vocab.distribution(zd[i, 0].astype(np.float64))
+        assert float(u[i, 0]) * q[x[i, 0]] > p[x[i, 0]] * (1 + 2.0 ** -25)  # rejected
+        assert q[x[i, 0]] - p[x[i, 0]] < 2.0 ** -36
+        u[i, 1] = np.float32(p[:x[i, 0]].sum() + 0.5 * p[x[i, 0]])
+    tokens, n = _verify_one_draft(rbp, z.astype(np.float64), zd.astype(np.float64), x, u)
+    assert (n == 1).all() and (tokens == x[:, 0]).all()
