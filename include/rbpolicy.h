@@ -557,8 +557,9 @@ int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
  * Its backward: dW_v (+)= scale * sum over {t: tokens_t = v, not masked} of dx_t.
  * Each row's sum runs over its tokens in batch order, in pieces that are then
  * added in order: fp32, no atomics on it.  (Up to 512 tokens by blocks that look
- * for equal ones; more are sorted, so that no time depends on how often a token
- * occurs.)
+ * for equal ones, where a frequent token's block sums alone; more are sorted and cut
+ * into slices of equal length, whose ends of a frequent token's run are joined by
+ * few blocks: 2^22 equal tokens take 1.2 times as long as a text's.)
  * dx      device [T, d], RBP_BF16 or RBP_F32 (dx_type); tokens, seq_of_token as in
  *         policy_embed_fwd (masked tokens and those outside [0, V) add nothing);
  * dW      device fp32 [V, d]: overwritten (rows without a token: 0), or added to

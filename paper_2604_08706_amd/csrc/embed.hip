@@ -245,64 +245,80 @@ struct Keys {
   }
 };
 
-// hist[tile][digit] of a pass.  (Counted by atomics where the pass before puts its
-// keys instead, a frequent token's take turns: 8 us more there, 4.6 for this launch.)
-template <int kItems>
+// hist[block][digit] of a pass: a block takes a tile, or `steps` consecutive ones (kMany; known
+// to be one, 0.2 us less a launch).  (Counted by
+// atomics where the pass before puts its keys instead, a frequent token's take turns: 8 us
+// more there, 4.6 for this launch.)
+template <int kItems, bool kMany>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Keys in, int64_t T, int shift,
-                                                                  int n_tiles,
+                                                                  int n_blocks, int steps,
                                                                   uint32_t* __restrict__ hist,
                                                                   Fill f) {
   __shared__ uint32_t bins[kBins];
-  if ((int)blockIdx.x >= n_tiles) return fill<kSortThreads>(f, blockIdx.x - n_tiles);
+  if ((int)blockIdx.x >= n_blocks) return fill<kSortThreads>(f, blockIdx.x - n_blocks);
   bins[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t t0 = (int64_t)blockIdx.x * (kSortThreads * kItems);
+  if constexpr (!kMany) steps = 1;
+  int64_t t0 = (int64_t)blockIdx.x * steps * (kSortThreads * kItems);
+  for (int step = 0; step < steps; ++step, t0 += kSortThreads * kItems) {
 #pragma unroll
-  for (int k = 0; k < kItems; ++k) {
-    const int64_t i = t0 + k * kSortThreads + threadIdx.x;
-    if (i < T) atomicAdd(&bins[digit_of(in.load(i), shift)], 1u);
+    for (int k = 0; k < kItems; ++k) {
+      const int64_t i = t0 + k * kSortThreads + threadIdx.x;
+      if (i < T) atomicAdd(&bins[digit_of(in.load(i), shift)], 1u);
+    }
   }
   __syncthreads();
   hist[(int64_t)blockIdx.x * kBins + threadIdx.x] = bins[threadIdx.x];
 }
 
-// One pass: every key of the tile to its place.  16384 tokens: 5 us, as the count
-// before it takes.
-template <int kItems>
+// One pass: every key of the block's tiles to its place, tile after tile.  16384 tokens: 5 us,
+// as the count before it takes.
+template <int kItems, bool kMany>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(
-    Keys in, int64_t T, int shift, const uint32_t* __restrict__ hist, int n_tiles,
+    Keys in, int64_t T, int shift, const uint32_t* __restrict__ hist, int n_blocks, int steps,
     uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out, Fill f) {
   constexpr int kTile = kSortThreads * kItems, kWaves = kSortThreads / 64;
   __shared__ uint32_t cnt[kWaves + 1][kBins];
   __shared__ uint32_t base[kBins], wave_sum[kBins / 64];
-  if ((int)blockIdx.x >= n_tiles) return fill<kSortThreads>(f, blockIdx.x - n_tiles);
+  if ((int)blockIdx.x >= n_blocks) return fill<kSortThreads>(f, blockIdx.x - n_blocks);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t t0 = (int64_t)blockIdx.x * kTile + wave * (64 * kItems);
-  const int live = T - t0 < kTile ? (int)(T - t0) : kTile;
+  if constexpr (!kMany) steps = 1;
+  int64_t t0 = (int64_t)blockIdx.x * steps * kTile + wave * (64 * kItems);
   uint32_t key[kItems], at[kItems], place[kItems];
+  auto load = [&] {
 #pragma unroll
-  for (int k = 0; k < kItems; ++k) {
-    const int64_t i = t0 + k * 64 + lane;
-    key[k] = i >= T ? 0u : in.load(i);
-    at[k] = i >= T || in.key == nullptr ? (uint32_t)i : in.at[i];
-  }
-  // this thread's bin: keys of it in all tiles, and in those before this one
+    for (int k = 0; k < kItems; ++k) {
+      const int64_t i = t0 + k * 64 + lane;
+      key[k] = i >= T ? 0u : in.load(i);
+      at[k] = i >= T || in.key == nullptr ? (uint32_t)i : in.at[i];
+    }
+  };
+  load();
+  // this thread's bin: keys of it in all blocks, and in those before this one
   uint32_t total = 0, before = 0;
 #pragma unroll 8
-  for (int b = 0; b < n_tiles; ++b) {
+  for (int b = 0; b < n_blocks; ++b) {
     const uint32_t h = hist[(int64_t)b * kBins + tid];
     total += h;
     before += b < (int)blockIdx.x ? h : 0u;
   }
   base[tid] = scan_bins(total, wave_sum) + before;
-  rank_tile<kItems, kWaves>(key, live, shift, cnt, place);
+  for (int step = 0;;) {
+    const int live = T - t0 < kTile ? (int)(T - t0) : kTile;
+    rank_tile<kItems, kWaves>(key, live, shift, cnt, place);
 #pragma unroll
-  for (int k = 0; k < kItems; ++k) {
-    if (k * 64 + lane >= live) continue;
-    const uint32_t digit = digit_of(key[k], shift);
-    const uint32_t to = base[digit] + cnt[wave][digit] + place[k];
-    key_out[to] = key[k];
-    at_out[to] = at[k];
+    for (int k = 0; k < kItems; ++k) {
+      if (k * 64 + lane >= live) continue;
+      const uint32_t digit = digit_of(key[k], shift);
+      const uint32_t to = base[digit] + cnt[wave][digit] + place[k];
+      key_out[to] = key[k];
+      at_out[to] = at[k];
+    }
+    if (++step == steps) break;
+    t0 += kTile;
+    load();
+    __syncthreads();  // base and cnt have been read
+    base[tid] += cnt[kWaves][tid];
   }
 }
 
@@ -571,10 +587,17 @@ __global__ void __launch_bounds__(256) few_kernel(const X* __restrict__ dx,
 
 __global__ void __launch_bounds__(kSortThreads) zero_kernel(Fill f) { fill<kSortThreads>(f, blockIdx.x); }
 
-// Keys per thread of a sort's tile: small tiles while their counts, which every tile
+// Keys per thread of a sort's tile: small tiles while their counts, which every block
 // reads, stay few.
 constexpr int64_t kShortSort = 65536;
 inline int sort_items(int64_t T) { return T <= kShortSort ? 2 : 8; }
+// Tiles of a block, so that those counts stay few however many tokens there are: every block
+// reads the 2 KB of every block (2^22 tokens of 64 bf16 in all 414 us, with a tile a block 555;
+// 2^23 596 / 1129; with 256 blocks 412 and 611).
+constexpr int kSortBlocks = 512;
+inline int sort_steps(int64_t T) {
+  return (int)rbp::ceil_div(rbp::ceil_div(T, kSortThreads * sort_items(T)), kSortBlocks);
+}
 // Tokens sorted in one launch, by counting, which takes their square: up to kRankMost
 // (4096 tokens of 896 bf16 17.2 us in all against 27.0 by tiles, 8192 25.3 / 30.4, 10007
 // 34.5 / 34.0), or all kRankKeys that fit beside the clearing of much of dW, which
@@ -591,17 +614,18 @@ inline int32_t slice_of(int64_t T, int n_chunks) {
   return s;
 }
 
-// What a workspace provides for: at least the slices and tiles of T tokens, and no fewer for
+// What a workspace provides for: at least the slices and sorting blocks of T tokens, and no fewer for
 // more tokens (a longer batch may be cut into fewer of them), so that one sized for the largest
 // batch serves all.
 inline int64_t most_slices(int64_t T, int n_chunks) {
   return std::min(rbp::ceil_div(T, kSliceLeast),
                   std::max(rbp::ceil_div(T, kSliceMost), (int64_t)(kSliceGroups / n_chunks + 1)));
 }
-inline int64_t most_tiles(int64_t T) {
+inline int64_t most_blocks(int64_t T) {
   return T <= kShortSort ? rbp::ceil_div(T, kSortThreads * 2)
-                         : std::max(rbp::ceil_div(T, kSortThreads * 8),
-                                    rbp::ceil_div(kShortSort, kSortThreads * 2));
+                         : std::clamp<int64_t>(rbp::ceil_div(T, kSortThreads * 8),
+                                               rbp::ceil_div(kShortSort, kSortThreads * 2),
+                                               kSortBlocks);
 }
 
 struct EmbedWs {
@@ -638,7 +662,7 @@ EmbedWs carve_embed(void* base, int64_t T, int32_t d) {
     w.key[k] = c.take<uint32_t>(n);
     w.at[k] = c.take<uint32_t>(n);
   }
-  w.hist = c.take<uint32_t>((size_t)most_tiles(T) * kBins);
+  w.hist = c.take<uint32_t>((size_t)most_blocks(T) * kBins);
   const int32_t dd = d < 8 ? 8 : d;
   w.part = c.take<float>((size_t)most_slices(T, chunks_of(dd)) * 2 * (size_t)dd);
   w.bytes = rbp::align_up(c.used, 256);
@@ -765,27 +789,31 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
     else
       go(std::integral_constant<int, 32>{});
   } else {
-    auto go = [&](auto items) {
+    auto go = [&](auto items, auto many) {
       constexpr int kItems = decltype(items)::value;
-      const int n_tiles = (int)rbp::ceil_div(T, kSortThreads * kItems);
+      constexpr bool kMany = decltype(many)::value;
+      const int steps = sort_steps(T);
+      const int n_blocks = (int)rbp::ceil_div(T, (int64_t)kSortThreads * kItems * steps);
       Keys in{tokens, seq_of_token, nullptr, nullptr, V};
       for (int p = 0; p < passes; ++p) {
         const int shift = p * kMaxDigit;
         Fill f = share();
-        hipLaunchKernelGGL(sort_count_kernel<kItems>, dim3(n_tiles + f.blocks), dim3(kSortThreads),
-                           0, s, in, T, shift, n_tiles, w.hist, f);
+        hipLaunchKernelGGL((sort_count_kernel<kItems, kMany>), dim3(n_blocks + f.blocks), dim3(kSortThreads),
+                           0, s, in, T, shift, n_blocks, steps, w.hist, f);
         f = share();
-        hipLaunchKernelGGL(sort_scatter_kernel<kItems>, dim3(n_tiles + f.blocks),
-                           dim3(kSortThreads), 0, s, in, T, shift, w.hist, n_tiles, w.key[p & 1],
-                           w.at[p & 1], f);
+        hipLaunchKernelGGL((sort_scatter_kernel<kItems, kMany>), dim3(n_blocks + f.blocks),
+                           dim3(kSortThreads), 0, s, in, T, shift, w.hist, n_blocks, steps,
+                           w.key[p & 1], w.at[p & 1], f);
         in.key = key = w.key[p & 1];
         in.at = at = w.at[p & 1];
       }
     };
     if (sort_items(T) == 2)
-      go(std::integral_constant<int, 2>{});
+      go(std::integral_constant<int, 2>{}, std::false_type{});
+    else if (sort_steps(T) == 1)
+      go(std::integral_constant<int, 8>{}, std::false_type{});
     else
-      go(std::integral_constant<int, 8>{});
+      go(std::integral_constant<int, 8>{}, std::true_type{});
   }
   RBP_CHECK_LAUNCH("policy_embed_bwd");
   with_lanes(d / 8, [&](auto lanes) {

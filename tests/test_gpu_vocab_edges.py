@@ -4,11 +4,19 @@ workspace for batches of every size, and other calls that the tests of each oper
 import numpy as np
 import pytest
 import torch
+from scipy.sparse import csr_matrix
 
 from gpu_util import require_gpu, to_np
 from oracle import vocab
 
 pytestmark = pytest.mark.gpu
+
+
+def _rows_summed(y, dx, V):
+    """fp64 [V, d] on the host: the sums of dx over equal y.  (Atomic 64-bit additions to one
+    row, as an indexed addition on the GPU makes them, take 20 s for 160000 of them.)"""
+    one = csr_matrix((np.ones(len(y)), (to_np(y), np.arange(len(y)))), shape=(V, len(y)))
+    return torch.from_numpy(one @ to_np(dx).astype(np.float64))
 
 
 def test_embedding_gradients_of_many_sizes_in_the_workspace_of_the_largest():
@@ -25,9 +33,8 @@ def test_embedding_gradients_of_many_sizes_in_the_workspace_of_the_largest():
         dW = torch.full((V, d), 7.0, device="cuda")
         print(f"[workspace] embed_bwd T={T}", flush=True)
         rbp.policy_embed_bwd(dx[:T], y[:T], None, dW, ws)
-        want = torch.zeros((V, d), dtype=torch.float64, device="cuda")
-        want.index_add_(0, y[:T].long(), dx[:T].double())
-        assert torch.equal(dW.double(), want)  # small integers: exact
+        # small integers: exact
+        assert torch.equal(dW.double().cpu(), _rows_summed(y[:T], dx[:T], V))
 
 
 def test_verification_of_a_shrinking_batch_in_one_workspace():
@@ -224,3 +231,28 @@ def test_a_remainder_below_the_sums_own_error_counts_as_none():
         u[i, 1] = np.float32(p[:x[i, 0]].sum() + 0.5 * p[x[i, 0]])
     tokens, n = _verify_one_draft(rbp, z.astype(np.float64), zd.astype(np.float64), x, u)
     assert (n == 1).all() and (tokens == x[:, 0]).all()
+
+
+@pytest.mark.parametrize("T,V,kind,acc", [
+    ((1 << 21) - 1, 300001, "skewed", True), ((1 << 21) + 1, 5000, "uniform", False),
+    ((1 << 21) + 4097, 300001, "skewed", False), (3145733, 5000, "equal", True),
+    ((1 << 22) + 5, 511, "uniform", True)])
+def test_embedding_gradient_of_more_tokens_than_the_sort_has_tiles_at_once(T, V, kind, acc):
+    """From 2^21 tokens on a sorting block takes two tiles and more, the last of them cut short or
+    empty.  Small integers: every sum is exact."""
+    rbp = require_gpu()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    if kind != "uniform":
+        y[torch.rand(T, generator=g, device="cuda") < (2.0 if kind == "equal" else 0.5)] = V // 3
+    seq = torch.randint(-1, 4, (T,), generator=g, device="cuda", dtype=torch.int32)
+    dx = torch.randint(-4, 5, (T, 8), generator=g, device="cuda").float()
+    dW = torch.randint(-9, 10, (V, 8), generator=g, device="cuda").float()
+    keep = seq >= 0
+    want = _rows_summed(y[keep], dx[keep], V) + (dW.double().cpu() if acc else 0.0)
+    ws = rbp.workspace(rbp.RBP_OP_EMBED_BWD, T, 8, V)
+    ws.fill_(255)
+    print(f"[sort] T={T} V={V} {kind} {acc}", flush=True)
+    rbp.policy_embed_bwd(dx, y, seq, dW, ws, accumulate_dW=acc)
+    assert torch.equal(dW.double().cpu(), want)

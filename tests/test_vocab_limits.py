@@ -64,3 +64,12 @@ def test_distillation_workspace_grows_with_tokens_and_entries(V):
     for T in (1, 2, 15, 16, 17, 63, 64, 65, 300, 5000):
         got = [rbp.rbp_workspace_bytes(rbp.RBP_OP_DISTILL, T, K, V) for K in range(1, 257)]
         assert all(a <= b for a, b in zip(got, got[1:])), (T, V)
+
+
+def test_what_sorting_keeps_of_its_blocks_stays_small():
+    """Every block reads the digit counts of all: at 2^30 tokens they had been 512 MB for each of
+    262144 blocks.  Beside two (key, position) pairs a token and two rows for 256 tokens the
+    workspace has room for 2 MB."""
+    for T in (1 << 20, (1 << 21) + 1, 1 << 24, 1 << 30):
+        got = rbp.rbp_workspace_bytes(rbp.RBP_OP_EMBED_BWD, T, 8, 1000)
+        assert got <= 16 * T + (T // 256 + 4097) * 2 * 8 * 4 + (1 << 21)
