@@ -713,6 +713,8 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   RBP_REQUIRE(std::isfinite(scale), RBP_EINVAL, "policy_embed_bwd: scale is not finite");
   RBP_REQUIRE(d % 8 == 0, RBP_EUNSUPPORTED, "policy_embed_bwd: d %% 8 != 0 (d = %d)", d);
   RBP_REQUIRE(T <= (int64_t(1) << 30), RBP_EUNSUPPORTED, "policy_embed_bwd: T above 2^30");
+  // (columns are counted in 32 bits up to the end of a chunk of 512)
+  RBP_REQUIRE(d <= INT32_MAX - 511, RBP_EUNSUPPORTED, "policy_embed_bwd: d above 2^31 - 512");
   RBP_REQUIRE(dW && (T == 0 || (dx && tokens)), RBP_EINVAL, "policy_embed_bwd: null pointer");
   RBP_REQUIRE(aligned(dW, 16) && aligned(dx, 16), RBP_EUNSUPPORTED,
               "policy_embed_bwd: dx and dW must be aligned to 16 bytes");

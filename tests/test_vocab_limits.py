@@ -6,7 +6,7 @@ import random
 import pytest
 
 import paper_2604_08706_amd as rbp
-from test_vocab_refusals import _distill, _verify
+from test_vocab_refusals import _distill, _embed_bwd, _verify
 
 LONGEST = 2 ** 31 - 1 - 2 ** 14
 
@@ -18,6 +18,14 @@ def test_rows_whose_last_tile_passes_31_bits_are_refused(call):
     """Indices beyond the row's end are formed before they are compared with it."""
     assert call(LONGEST) == rbp.RBP_EWORKSPACE  # goes on to the next check
     assert call(LONGEST + 1) == call(2 ** 31 - 1) == rbp.RBP_EUNSUPPORTED
+
+
+def test_rows_whose_last_chunk_passes_31_bits_are_refused():
+    """The gradient counts columns up to the end of a chunk of 512."""
+    for T in (1, 60):
+        assert _embed_bwd(T=T, d=2 ** 31 - 512, ws_bytes=0) == rbp.RBP_EWORKSPACE
+        for d in (2 ** 31 - 504, 2 ** 31 - 8):
+            assert _embed_bwd(T=T, d=d, ws_bytes=0) == rbp.RBP_EUNSUPPORTED
 
 
 def _growing(op, sizes, d, V):
