@@ -568,8 +568,8 @@ int policy_embed_fwd(const uint16_t* table, const int32_t* tokens,
  * ws      device, >= rbp_workspace_bytes(RBP_OP_EMBED_BWD, T, d, V).
  * Errors: RBP_EINVAL (null pointers, T < 0, d < 1, V < 1, an unknown dx_type, scale
  *         not finite, ws not aligned to 16 bytes); RBP_EUNSUPPORTED (d % 8 != 0, dx
- *         or dW not aligned to 16 bytes, T above 2^30, d above 2^31 - 512);
- *         RBP_EWORKSPACE.
+ *         or dW not aligned to 16 bytes, T above 2^30, d above 2^31 - 512, T * d
+ *         above 2^37); RBP_EWORKSPACE.
  */
 int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
                      const int32_t* seq_of_token, int64_t T, int32_t d, int32_t V,

@@ -495,7 +495,9 @@ __global__ void __launch_bounds__(256) run_join_kernel(Sorted in, int n_chunks, 
 // so 512 equal tokens take 23 against 14 (1024 would 43 against 19), and clearing
 // more than kFewClear is done sooner beside the sort (2.2 GB 379 against 391, but
 // 545 MB 102 against 99).
+// (A launch has less than 2^32 threads, 4 of them for 8 elements of dx: kFewPieces.)
 constexpr int kFewMost = 512, kFewFill = 2048;
+constexpr int64_t kFewPieces = 1 << 29;
 constexpr int64_t kFewClear = 1 << 26;  // float4 of dW
 template <class X, int kLanes, bool kAdd>
 __global__ void __launch_bounds__(256) few_kernel(const X* __restrict__ dx,
@@ -715,6 +717,8 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
   RBP_REQUIRE(T <= (int64_t(1) << 30), RBP_EUNSUPPORTED, "policy_embed_bwd: T above 2^30");
   // (columns are counted in 32 bits up to the end of a chunk of 512)
   RBP_REQUIRE(d <= INT32_MAX - 511, RBP_EUNSUPPORTED, "policy_embed_bwd: d above 2^31 - 512");
+  RBP_REQUIRE(T * (d / 8) <= (int64_t(1) << 34), RBP_EUNSUPPORTED,
+              "policy_embed_bwd: T * d above 2^37");
   RBP_REQUIRE(dW && (T == 0 || (dx && tokens)), RBP_EINVAL, "policy_embed_bwd: null pointer");
   RBP_REQUIRE(aligned(dW, 16) && aligned(dx, 16), RBP_EUNSUPPORTED,
               "policy_embed_bwd: dx and dW must be aligned to 16 bytes");
@@ -747,7 +751,7 @@ extern "C" int policy_embed_bwd(const void* dx, int dx_type, const int32_t* toke
     RBP_CHECK_LAUNCH("policy_embed_bwd");
     return RBP_OK;
   }
-  if (T <= kFewMost && n_fill <= kFewClear) {
+  if (T <= kFewMost && n_fill <= kFewClear && T * (d / 8) < kFewPieces) {
     with_lanes(d / 8, [&](auto lanes) {
       constexpr int kLanes = decltype(lanes)::value;
       const int n_chunks = (int)rbp::ceil_div(d / 8, kLanes);

@@ -256,3 +256,24 @@ def test_embedding_gradient_of_more_tokens_than_the_sort_has_tiles_at_once(T, V,
     print(f"[sort] T={T} V={V} {kind} {acc}", flush=True)
     rbp.policy_embed_bwd(dx, y, seq, dW, ws, accumulate_dW=acc)
     assert torch.equal(dW.double().cpu(), want)
+
+
+def test_embedding_gradient_of_few_rows_that_are_very_long():
+    """512 rows of 2^24 columns and some, 17 GB: a block for each chunk of each row would be more
+    threads than a launch has.  Small integers: exact."""
+    rbp = require_gpu()
+    T, V, d = 512, 2, (1 << 24) + 8
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    line = torch.randint(-3, 4, (d,), generator=g, device="cuda").bfloat16()
+    times = torch.randint(-2, 3, (T,), generator=g, device="cuda").bfloat16()
+    y = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    dx = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
+    for t in range(T):
+        torch.mul(line, times[t], out=dx[t])
+    dW = torch.full((V, d), 7.0, device="cuda")
+    print("[few] 512 long rows", flush=True)
+    rbp.policy_embed_bwd(dx, y, None, dW, rbp.workspace(rbp.RBP_OP_EMBED_BWD, T, d, V),
+                         accumulate_dW=True)
+    for v in range(V):
+        assert torch.equal(dW[v], 7.0 + line.float() * times[y == v].float().sum())

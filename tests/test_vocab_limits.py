@@ -28,6 +28,13 @@ def test_rows_whose_last_chunk_passes_31_bits_are_refused():
             assert _embed_bwd(T=T, d=d, ws_bytes=0) == rbp.RBP_EUNSUPPORTED
 
 
+def test_gradients_beyond_what_a_launch_counts_are_refused():
+    for T, d in ((1 << 30, 136), ((1 << 24) + 1, 1 << 13), (512, (1 << 28) + 8)):
+        assert _embed_bwd(T=T, d=d, ws_bytes=0) == rbp.RBP_EUNSUPPORTED
+    for T, d in ((1 << 30, 128), (1 << 24, 1 << 13), (512, 1 << 28)):
+        assert _embed_bwd(T=T, d=d, ws_bytes=0) == rbp.RBP_EWORKSPACE
+
+
 def _growing(op, sizes, d, V):
     """rbp_workspace_bytes over growing n."""
     got = [rbp.rbp_workspace_bytes(op, n, d, V) for n in sizes]
