@@ -135,6 +135,12 @@ void* stream(PyObject* o) {
   return p;
 }
 
+// A size that the C ABI takes in 32 bits.
+int32_t size32(int64_t n, const char* name) {
+  if (n > INT32_MAX) raise(PyExc_ValueError, "%s has a size above 2^31 - 1", name);
+  return (int32_t)n;
+}
+
 // Throws unless the tensor (None is passed over) lies on the current device,
 // whose stream the call uses.
 void here(PyObject* o, const char* name) {
@@ -153,11 +159,12 @@ struct Rows {
 };
 Rows rows(PyObject* o, const char* name, int64_t dims) {
   const at::Tensor& t = tensor(o, name);
+  if (t.dim() != dims) raise(PyExc_ValueError, "%s has the wrong number of dimensions", name);
+  for (int64_t k = 0; k < dims; ++k) size32(t.size(k), name);
   if (!t.is_cuda()) raise(PyExc_ValueError, "%s must be a device tensor", name);
   here(o, name);
   if (t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat)
     raise(PyExc_TypeError, "%s must be torch.bfloat16 or torch.float32", name);
-  if (t.dim() != dims) raise(PyExc_ValueError, "%s has the wrong number of dimensions", name);
   const int64_t V = t.size(dims - 1);
   bool even = V <= 1 || t.stride(dims - 1) == 1;
   int64_t ld = -1, n = 1;  // row stride, rows of the dimensions inside the present one
@@ -488,6 +495,7 @@ PyObject* hist_accumulate(const Args& a) {  // values hist lo stream
 PyObject* embed_fwd(const Args& a) {  // table tokens seq out scale stream
   int64_t V, d;
   sizes_2d(a[0], "table", V, d);
+  size32(V, "table"), size32(d, "table");
   const int64_t T = numel_of(a[1], "tokens");
   const uint16_t* table = bf16(a[0], "table", V * d);
   const int32_t *tok = i32(a[1], "tokens", T), *seq = i32_or_null(a[2], "seq_of_token", T);
@@ -502,6 +510,7 @@ PyObject* embed_fwd(const Args& a) {  // table tokens seq out scale stream
 PyObject* embed_bwd(const Args& a) {  // dx tokens seq dW ws scale accumulate stream
   int64_t V, d;
   sizes_2d(a[3], "dW", V, d);
+  size32(V, "dW"), size32(d, "dW");
   const int64_t T = numel_of(a[1], "tokens");
   const at::Tensor& x = tensor(a[0], "dx");
   const bool wide = x.scalar_type() == at::kFloat;
@@ -558,7 +567,8 @@ PyObject* distill_fwd_bwd(const Args& a) {
   int64_t Ti, K;
   sizes_2d(a[1], "teacher_ids", Ti, K);
   if (Ti != T) raise(PyExc_ValueError, "%s must be [T, K]", "teacher_ids");
-  const int64_t B = numel_of(a[5], "seq_len");
+  size32(K, "teacher_ids");
+  const int64_t B = size32(numel_of(a[5], "seq_len"), "seq_len");
   const int32_t* ids = i32(a[1], "teacher_ids", T * K);
   const float *lt = f32(a[2], "teacher_logits", T * K), *mass = f32_or_null(a[3], "teacher_lse", T);
   const int32_t *seq = i32(a[4], "seq_of_token", T), *len = i32(a[5], "seq_len", B);

@@ -4,6 +4,7 @@ sizes of their workspaces (CPU: the C ABI, stopped by its own checks before any 
 import random
 
 import pytest
+import torch
 
 import paper_2604_08706_amd as rbp
 from test_vocab_refusals import _distill, _embed_bwd, _verify
@@ -88,3 +89,22 @@ def test_what_sorting_keeps_of_its_blocks_stays_small():
     for T in (1 << 20, (1 << 21) + 1, 1 << 24, 1 << 30):
         got = rbp.rbp_workspace_bytes(rbp.RBP_OP_EMBED_BWD, T, 8, 1000)
         assert got <= 16 * T + (T // 256 + 4097) * 2 * 8 * 4 + (1 << 21)
+
+
+def test_sizes_that_do_not_fit_the_c_abi_are_refused():
+    """2^32 + 10 rows, columns or sequences were taken for 10.  (Tensors without memory.)"""
+    many = 2 ** 32 + 10
+
+    def t(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    i, bf = t(4, dtype=torch.int32), torch.bfloat16
+    with pytest.raises(ValueError, match="2\\^31"):
+        rbp.policy_embed_fwd(t(many, 8, dtype=bf), i, None, t(4, 8, dtype=bf))
+    with pytest.raises(ValueError, match="2\\^31"):
+        rbp.policy_embed_bwd(t(4, 8), i, None, t(many, 8), None)
+    for shape in ((1, 1, many), (many, 1, 4), (1, many, 4)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            rbp.policy_verify_drafts(t(*shape), None, None, None, i, i, i, i, None)
+    with pytest.raises(ValueError, match="2\\^31"):
+        rbp.policy_distill_fwd_bwd(t(4, many), i, i, None, i, i, 1, i, i, i, None, None)
