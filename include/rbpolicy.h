@@ -607,8 +607,9 @@ int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
  * 1e-12 of u.  Where a token is drawn from max(p_a - q_a, 0), whose total R is a
  * difference of such sums, that is within 2^-25 (half a step of u) + 1e-12 / R; and
  * a total of 2^-36 or less counts as 0 (such a rejection has that probability).
- * out_logp beside draft_logits comes from 32-bit sums for accepted drafts (off by at
- * most 5e-6 at V = 2^18), from 64-bit ones else.
+ * out_logp beside draft_logits comes from sums of 32-bit exponentials for accepted
+ * drafts (off by at most 5.5 2^-24, half a step of a log-prob of -5.5), from 64-bit
+ * ones else.
  * Logits of -infinity have probability 0.  A row of logits with a NaN,
  * with +infinity, or with -infinity only has no distribution: a draft at such a
  * position of the policy's is rejected, and drawing there emits token -1 with a

@@ -202,11 +202,12 @@ struct Place {
   const X* row;
   uint32_t row_id;
   int seg;
+  bool kept;  // a row of the policy's whose draft may be accepted
 };
 template <bool kDrafts, class X>
 __device__ __forceinline__ Place<X> place_of(const X* logits, const X* draft_logits, const Args& a,
                                              int64_t n_items) {
-  Place<X> p{nullptr, 0, 0};
+  Place<X> p{nullptr, 0, 0, false};
   // (rows times segments may pass 31 bits, rows may not)
   const int64_t item = (int64_t)blockIdx.x * (blockDim.x >> 6) +
                        __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -219,6 +220,7 @@ __device__ __forceinline__ Place<X> place_of(const X* logits, const X* draft_log
   const int32_t n = a.drafts(b);  // (negative: no row)
   if (k <= a.K) {
     if (k <= n) p.row = logits + (b * (a.K + 1) + k) * a.ld;
+    p.kept = k < n;
   } else if constexpr (kDrafts) {
     const int at = k - a.K - 1;
     if (at < n) p.row = draft_logits + (b * a.K + at) * a.ld_draft;
@@ -241,8 +243,12 @@ constexpr double kUnsure = 0x1p-16;
 struct Rough {
   float m = -INFINITY;
   double s = 0.0;
+  float k2, slack;
+  __device__ __forceinline__ explicit Rough(const Args& a)
+      : k2((float)a.k2), slack(fminf(kRoughSlack / k2, 1e30f)) {}
+  __device__ __forceinline__ double sum() const { return s; }
   template <int N>
-  __device__ __forceinline__ void add(const float (&x)[N], float k2, float slack) {
+  __device__ __forceinline__ void add(const float (&x)[N]) {
     float top = x[0];
 #pragma unroll
     for (int k = 1; k < N; ++k) top = fmaxf(top, x[k]);
@@ -261,6 +267,60 @@ struct Rough {
     s += (double)e[0];
   }
 };
+
+// The same for the policy's rows whose drafts may be accepted, since their sums are in those
+// tokens' log-probs, without the roundings of the argument d k2.
+// - The difference d loses nothing: the reference is 0 while the largest logit is within 64
+//   powers of two of it, else that logit, which those that matter differ from by less than half.
+// - What the product of d and k2's 32 bits loses (l: 2^l is 1 + l ln 2) is summed beside it, in c.
+// - What k2's 32 bits lose, `lo` of it and at most 2^-25, counts lo d for the largest of a piece
+//   and its other elements alike: weighted, those are 3 powers of two less at most.
+// So a sum is off by its exponentials' errors (1.43 2^-24 at most, over all arguments), three
+// additions of eight and 1.1 2^-24 for the third point: 5.5 2^-24 of itself at most.
+struct Fine {
+  static constexpr float kNear = 64.0f, kGone = -160.0f;  // in powers of two
+  float m = -INFINITY, top = -INFINITY, c = 0.0f;
+  double s = 0.0, k2;
+  float hi, lo, near, gone;
+  __device__ __forceinline__ explicit Fine(const Args& a)
+      : k2(a.k2), hi((float)k2), lo((float)(k2 - (double)hi)), near(kNear / hi), gone(kGone / hi) {}
+  // (a row with a NaN has no sum; the clamp below lets none through)
+  __device__ __forceinline__ double sum() const {
+    return top != top ? (double)NAN : fma((double)c, kLn2, s);
+  }
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N]) {
+    float largest = x[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) largest = __builtin_elementwise_maximum(largest, x[k]);
+    top = __builtin_elementwise_maximum(top, largest);
+    if (largest > m + near) {
+      const float to = fabsf(largest) <= near ? 0.0f : largest;
+      if (m != -INFINITY) {
+        const double f = exp2_d(((double)m - (double)to) * k2);
+        s *= f;
+        c *= (float)f;
+      }
+      m = to;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float e[N], l[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float d = fmaxf(x[k] - ref, gone), y = d * hi;
+      l[k] = fmaf(d, hi, -y);
+      e[k] = rbp::lp::exp2_hw(y);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) c = fmaf(e[k], l[k], c);
+#pragma unroll
+    for (int w = N / 2; w >= 1; w /= 2)
+#pragma unroll
+      for (int k = 0; k < w; ++k) e[k] += e[k + w];
+    c = fmaf(e[0], fmaxf(largest - ref, gone) * lo, c);
+    s += (double)e[0];
+  }
+};
 template <class X>
 __global__ void __launch_bounds__(kStatsThreads) rough_kernel(const X* __restrict__ logits,
                                                               const X* __restrict__ draft_logits,
@@ -271,33 +331,37 @@ __global__ void __launch_bounds__(kStatsThreads) rough_kernel(const X* __restric
   const int lane = threadIdx.x & 63;
   const Row<X> r(place.row, a.V);
   const Segment<X> g(r, place.seg, a.log_segments);
-  const float k2 = (float)a.k2, slack = fminf(kRoughSlack / k2, 1e30f);
-  Rough o;
-  for (int32_t c = g.p0 + lane; c < g.p1; c += kBatch * 64) {
-    uint4 v[kBatch];
+  auto run = [&](auto o) {
+    for (int32_t c = g.p0 + lane; c < g.p1; c += kBatch * 64) {
+      uint4 v[kBatch];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      if (c + i * 64 < g.p1) v[i] = *reinterpret_cast<const uint4*>(place.row + r.at(c + i * 64));
+      for (int i = 0; i < kBatch; ++i)
+        if (c + i * 64 < g.p1) v[i] = *reinterpret_cast<const uint4*>(place.row + r.at(c + i * 64));
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      if (c + i * 64 < g.p1) {
-        float x[E];
-        unpack(v[i], x);
-        o.add(x, k2, slack);
-      }
-  }
-  const int32_t loose = r.loose(lane);
-  if (loose >= 0 && (loose < r.head ? place.seg == 0 : place.seg == a.segments - 1)) {
-    const float x[1] = {value(place.row[loose])};
-    o.add(x, k2, slack);
-  }
-  float M = o.m;
+      for (int i = 0; i < kBatch; ++i)
+        if (c + i * 64 < g.p1) {
+          float x[E];
+          unpack(v[i], x);
+          o.add(x);
+        }
+    }
+    const int32_t loose = r.loose(lane);
+    if (loose >= 0 && (loose < r.head ? place.seg == 0 : place.seg == a.segments - 1)) {
+      const float x[1] = {value(place.row[loose])};
+      o.add(x);
+    }
+    float M = o.m;
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-  double s = o.s;
-  if (o.m != M) s *= exp2_d(((double)o.m - (double)M) * a.k2);
-  s = wave_sum(s);
-  if (lane == 0) a.parts[(int64_t)place.row_id * a.segments + place.seg] = Part{s, M, 0.0f};
+    for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+    double s = o.sum();
+    if (o.m != M) s *= exp2_d(((double)o.m - (double)M) * a.k2);
+    s = wave_sum(s);
+    if (lane == 0) a.parts[(int64_t)place.row_id * a.segments + place.seg] = Part{s, M, 0.0f};
+  };
+  if (place.kept)
+    run(Fine(a));
+  else
+    run(Rough(a));
 }
 
 // A wave per segment of a row, in 64 bits: bound by its 13 64-bit operations a logit

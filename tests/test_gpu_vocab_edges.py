@@ -277,3 +277,65 @@ def test_embedding_gradient_of_few_rows_that_are_very_long():
                          accumulate_dW=True)
     for v in range(V):
         assert torch.equal(dW[v], 7.0 + line.float() * times[y == v].float().sum())
+
+
+def _accepted(rbp, z, x, tau):
+    """Log-probs of drafts from the policy's own rows z [B, K + 1, V], all of them accepted."""
+    B, K1, V = z.shape
+    tokens = torch.empty((B, K1), dtype=torch.int32, device="cuda")
+    logp, n = torch.empty((B, K1), device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    rbp.policy_verify_drafts(z, z[:, :K1 - 1].contiguous(), torch.from_numpy(x).cuda(), None,
+                             torch.full((B, K1), 0.5, device="cuda"), tokens, logp, n,
+                             rbp.workspace(rbp.RBP_OP_VERIFY, B, K1 - 1, V), temperature=tau)
+    assert (n == K1).all() and np.array_equal(to_np(tokens)[:, :K1 - 1], x)
+    return to_np(logp)[:, :K1 - 1].astype(np.float64)
+
+
+# exponentials off by 1.43 2^-24, three additions of eight and what is left of the temperature's
+# rounding, of the sum; then the output's rounding, half a step of its value
+def _close(got, want):
+    return np.all(np.abs(got - want) <= 5.5 * 2.0 ** -24 + 2.0 ** -24 * np.abs(want) + 1e-9)
+
+
+def test_log_probs_of_accepted_drafts_over_a_flat_vocabulary():
+    """Equal logits that hold 0.8 between them, the first 256 of every 2048 nearly 8 powers of two
+    below: a rounding of the others' distance from those would be the same for all, 6e-7 at this
+    temperature.  The draft is a token that holds the rest."""
+    rbp = require_gpu()
+    B, V, tau = 12, 1 << 17, 2.5
+    low, flat = float(np.float32(-3.1)), float(np.float32(10.718529))
+    z = np.full((B, 2, V), flat)
+    z.reshape(B, 2, -1, 2048)[..., :256] = low
+    top = float(np.float32(flat + tau * np.log(V * 7 / 8 / 4)))
+    x = (256 + 2048 * np.arange(B) + 5 * np.arange(B)).astype(np.int32)[:, None]
+    for i in range(B):
+        z[i, :, x[i, 0]] = top
+    rest = (V * 7 / 8 - 1) * np.exp((flat - top) / tau) + V / 8 * np.exp((low - top) / tau)
+    got = _accepted(rbp, torch.from_numpy(z).float().cuda(), x, tau)
+    print("[log-probs] largest error", np.abs(got + np.log1p(rest)).max())
+    assert _close(got, -np.log1p(rest))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0.0, 50.0, -55.0, 1e3, -1e5])
+@pytest.mark.parametrize("tau,sd", [(1.0, 3.0), (1.3, 20.0), (0.2, 0.5)])
+def test_log_probs_of_accepted_drafts_wherever_the_logits_lie(dtype, offset, tau, sd):
+    """Rows around 0, whose reference is 0, beside the borders where it is not, and far away; ends
+    of a row masked by -infinity and by the type's lowest value."""
+    rbp = require_gpu()
+    rng = np.random.default_rng(int(abs(offset) + 10 * sd))
+    B, K, V = 3, 2, 20011
+    tau = float(np.float32(tau))
+    z = torch.from_numpy(rng.standard_normal((B, K + 1, V)) * sd + offset).to(dtype)
+    z[1, :, :9000] = -np.inf
+    z[2, :, 11000:] = torch.finfo(dtype).min
+    z[0, 0, :64] = -2e4 if offset > -1e5 else -3e5  # a first piece far below the others
+    zd = z.double().numpy()
+    x = np.zeros((B, K), np.int32)
+    want = np.zeros((B, K))
+    for i in range(B):
+        for k in range(K):
+            p = vocab.distribution(zd[i, k], tau)
+            x[i, k] = vocab.draw(p, rng.random())
+            want[i, k] = np.log(p[x[i, k]])
+    assert _close(_accepted(rbp, z.cuda(), x, tau), want)
