@@ -648,7 +648,8 @@ int policy_verify_drafts(const void* logits, const void* draft_logits, int logit
  *         (seq_of_token < 0) has KL 0 and a zero gradient, whatever its logits and
  *         teacher hold.  So does a token whose teacher has no entry, or entries of
  *         -infinity only.  An id >= V whose p_k is not 0 makes its token's KL NaN (and
- *         no gradient of its own);
+ *         no gradient of its own); so do logits of -infinity only, with +infinity or
+ *         with a NaN, and the row's gradient is NaN with it;
  * kl      device fp32 [T]: KL_t, overwritten;
  * loss_accum device fp32 [1] and stats device fp32 [2] are ACCUMULATED (+=):
  *         stats = {tokens not masked that have a teacher, sum of their KL_t};

@@ -603,7 +603,8 @@ inline int sort_steps(int64_t T) {
 // Tokens sorted in one launch, by counting, which takes their square: up to kRankMost
 // (4096 tokens of 896 bf16 17.2 us in all against 27.0 by tiles, 8192 25.3 / 30.4, 10007
 // 34.5 / 34.0), or all kRankKeys that fit beside the clearing of much of dW, which
-// hides it (10007 tokens, 545 MB 111 / 134).
+// hides it (8500 to 12288 tokens beside 272 MB 65 to 68 us against 71 to 76, 545 MB 110 to 112 /
+// 116 to 119, 934 MB 183 to 189 / 187 to 191).
 constexpr int kRankMost = 8192;
 constexpr int64_t kBesideFill = 1 << 24;  // float4 of dW
 

@@ -339,3 +339,26 @@ def test_log_probs_of_accepted_drafts_wherever_the_logits_lie(dtype, offset, tau
             x[i, k] = vocab.draw(p, rng.random())
             want[i, k] = np.log(p[x[i, k]])
     assert _close(_accepted(rbp, z.cuda(), x, tau), want)
+
+
+@pytest.mark.parametrize("V", [300, 20000])
+def test_divergence_from_rows_without_a_distribution(V):
+    """Logits of -infinity only, with +infinity or a NaN: the divergence and the row's gradient are
+    NaN, and the rows beside them as they would be."""
+    rbp = require_gpu()
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((5, V)).astype(np.float32)
+    ids = rng.integers(0, V, (5, 6)).astype(np.int32)
+    lt = rng.standard_normal((5, 6)).astype(np.float32)
+    z[1], z[2, V // 2], z[3, 5] = -np.inf, np.inf, np.nan
+    kl, loss, stats = (torch.zeros(n, device="cuda") for n in (5, 1, 2))
+    dz = torch.zeros((5, V), device="cuda")
+    rbp.policy_distill_fwd_bwd(torch.from_numpy(z).cuda(), torch.from_numpy(ids).cuda(),
+                               torch.from_numpy(lt).cuda(), None,
+                               torch.zeros(5, dtype=torch.int32, device="cuda"),
+                               torch.ones(1, dtype=torch.int32, device="cuda"), 1, kl, loss, stats,
+                               dz, rbp.workspace(rbp.RBP_OP_DISTILL, 5, 6, V))
+    assert kl[1:4].isnan().all() and dz[1:4].isnan().all() and stats[0].item() == 5
+    wkl, _, _, wdz = vocab.distill(z[[0, 4]], ids[[0, 4]], lt[[0, 4]], None, [0, 0], [1], 1)
+    assert np.abs(to_np(kl[[0, 4]]) - wkl).max() < 2e-5
+    assert np.abs(to_np(dz[[0, 4]]) - wdz).max() < 1e-6
