@@ -238,7 +238,8 @@ constexpr float kRoughSlack = 8.0f;
 // probabilities, |y| is at most log2 V + 2 kRoughSlack (the entropy bounds the distance
 // from the largest logit; the reference lags behind it, and moves), so the sum of a row
 // of 2^18 tokens is off by 5e-6 of itself at most, one of 2^31 by 7e-6, and p / q by
-// less than kUnsure.  Bound by HBM: 576 rows of 152064 bf16 32 us (5.4 TB/s).
+// less than kUnsure.  Bound by HBM: 576 rows of 152064 bf16 32 us (5.4 TB/s), 34 with 256 of
+// them summed as the struct after this one does.
 constexpr double kUnsure = 0x1p-16;
 struct Rough {
   float m = -INFINITY;
