@@ -540,7 +540,7 @@ int rb_hist_accumulate(const int32_t* values, int64_t n, int32_t lo, int32_t n_b
                        int64_t* hist, void* stream);
 
 /*
- * Embedding lookup: out_t = scale * table[tokens_t], rounded to bf16 once.
+ * Embedding lookup: out_t = scale * table[tokens_t], formed in fp32 and rounded to bf16.
  * table   device bf16 [V, d] (W where the head is tied); tokens device int32 [T];
  * seq_of_token device int32 [T] or NULL: a negative entry masks the token (a zero
  *         row); a token outside [0, V) that is not masked gives a row of NaN;
@@ -608,7 +608,7 @@ int policy_embed_bwd(const void* dx, int dx_type, const int32_t* tokens,
  * difference of such sums, that is within 2^-25 (half a step of u) + 1e-12 / R; and
  * a total of 2^-36 or less counts as 0 (such a rejection has that probability).
  * out_logp beside draft_logits comes from sums of 32-bit exponentials for accepted
- * drafts (off by at most 5.5 2^-24, half a step of a log-prob of -5.5), from 64-bit
+ * drafts (off by at most 6.6 2^-24, half a step of a log-prob of -6.6), from 64-bit
  * ones else.
  * Logits of -infinity have probability 0.  A row of logits with a NaN,
  * with +infinity, or with -infinity only has no distribution: a draft at such a

@@ -274,10 +274,10 @@ struct Rough {
 // - The difference d loses nothing: the reference is 0 while the largest logit is within 64
 //   powers of two of it, else that logit, which those that matter differ from by less than half.
 // - What the product of d and k2's 32 bits loses (l: 2^l is 1 + l ln 2) is summed beside it, in c.
-// - What k2's 32 bits lose, `lo` of it and at most 2^-25, counts lo d for the largest of a piece
-//   and its other elements alike: weighted, those are 3 powers of two less at most.
+// - What k2's 32 bits lose, `lo`, up to 2^-24 of it, counts lo d for the largest of a piece and
+//   its other elements alike: weighted, those are 3 powers of two less at most.
 // So a sum is off by its exponentials' errors (1.43 2^-24 at most, over all arguments), three
-// additions of eight and 1.1 2^-24 for the third point: 5.5 2^-24 of itself at most.
+// additions of eight (3 2^-24) and 3 ln 2 2^-24 for the third point: 6.6 2^-24 of itself at most.
 struct Fine {
   static constexpr float kNear = 64.0f, kGone = -160.0f;  // in powers of two
   float m = -INFINITY, top = -INFINITY, c = 0.0f;

@@ -291,10 +291,12 @@ def _accepted(rbp, z, x, tau):
     return to_np(logp)[:, :K1 - 1].astype(np.float64)
 
 
-# exponentials off by 1.43 2^-24, three additions of eight and what is left of the temperature's
-# rounding, of the sum; then the output's rounding, half a step of its value
+# Of the sum: exponentials off by 1.43 2^-24, three additions of eight, 2^-24 each, and what is
+# left of the rounding of log2 e / temperature, 2^-24 of it, on elements that lie (weighted) log2 8
+# powers of two below the largest of their eight at most: 3 ln 2 2^-24.  Then the output's rounding,
+# half a step of its value.
 def _close(got, want):
-    return np.all(np.abs(got - want) <= 5.5 * 2.0 ** -24 + 2.0 ** -24 * np.abs(want) + 1e-9)
+    return np.all(np.abs(got - want) <= (1.43 + 3 + 3 * np.log(2)) * 2.0 ** -24 + 2.0 ** -24 * np.abs(want) + 1e-9)
 
 
 def test_log_probs_of_accepted_drafts_over_a_flat_vocabulary():
