@@ -272,7 +272,8 @@ struct Rough {
 // The same for the policy's rows whose drafts may be accepted, since their sums are in those
 // tokens' log-probs, without the roundings of the argument d k2.
 // - The difference d loses nothing: the reference is 0 while the largest logit is within 64
-//   powers of two of it, else that logit, which those that matter differ from by less than half.
+//   powers of two of it, else a logit at most 32 below the largest: those that matter differ
+//   from it by less than half of it.
 // - What the product of d and k2's 32 bits loses (l: 2^l is 1 + l ln 2) is summed beside it, in c.
 // - What k2's 32 bits lose, `lo`, up to 2^-24 of it, counts lo d for the largest of a piece and
 //   its other elements alike: weighted, those are 3 powers of two less at most.
@@ -281,6 +282,7 @@ struct Rough {
 struct Fine {
   static constexpr float kNear = 64.0f, kGone = -160.0f;  // in powers of two
   float m = -INFINITY, top = -INFINITY, c = 0.0f;
+  float limit = -INFINITY;  // a logit above it moves the reference
   double s = 0.0, k2;
   float hi, lo, near, gone;
   __device__ __forceinline__ explicit Fine(const Args& a)
@@ -295,7 +297,7 @@ struct Fine {
 #pragma unroll
     for (int k = 1; k < N; ++k) largest = __builtin_elementwise_maximum(largest, x[k]);
     top = __builtin_elementwise_maximum(top, largest);
-    if (largest > m + near) {
+    if (largest > limit) {
       const float to = fabsf(largest) <= near ? 0.0f : largest;
       if (m != -INFINITY) {
         const double f = exp2_d(((double)m - (double)to) * k2);
@@ -303,6 +305,7 @@ struct Fine {
         c *= (float)f;
       }
       m = to;
+      limit = to == 0.0f ? near : to + 0.5f * near;
     }
     const float ref = m == -INFINITY ? 0.0f : m;
     float e[N], l[N];

@@ -318,6 +318,28 @@ def test_log_probs_of_accepted_drafts_over_a_flat_vocabulary():
     assert _close(got, -np.log1p(rest))
 
 
+def test_log_probs_of_accepted_drafts_where_a_row_begins_far_below_zero():
+    """The first 256 of every 2048 logits are nearly 64 powers of two below the others, which lie
+    beside 0: their difference from those would be rounded to 2^-18, by the same for all."""
+    rbp = require_gpu()
+    B, V = 12, 1 << 17
+    low = np.float32(-46.0)
+    near = (np.float32(-1.71) + np.arange(4000, dtype=np.float32) * np.float32(2.0 ** -23))
+    lost = np.abs((near - low).astype(np.float64) - (near.astype(np.float64) - float(low)))
+    flat = float(near[lost.argmax()])
+    assert lost.max() > 1.8e-6
+    z = np.full((B, 2, V), flat)
+    z.reshape(B, 2, -1, 2048)[..., :256] = low
+    x = (256 + 2053 * np.arange(B)).astype(np.int32)[:, None]
+    top = float(np.float32(flat + np.log(V * 7 / 8 / 4)))
+    for i in range(B):
+        z[i, :, x[i, 0]] = top
+    rest = (V * 7 / 8 - 1) * np.exp(flat - top) + V / 8 * np.exp(float(low) - top)
+    got = _accepted(rbp, torch.from_numpy(z).float().cuda(), x, 1.0)
+    print("[log-probs] largest error", np.abs(got + np.log1p(rest)).max())
+    assert _close(got, -np.log1p(rest))
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("offset", [0.0, 50.0, -55.0, 1e3, -1e5])
 @pytest.mark.parametrize("tau,sd", [(1.0, 3.0), (1.3, 20.0), (0.2, 0.5)])
